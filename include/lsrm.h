@@ -305,6 +305,96 @@ lsrm_status lsrm_nsa_backward(const lsrm_nsa_params *p, const uint16_t *d_q, con
                               uint16_t *d_dk, uint16_t *d_dv, void *d_ws, size_t ws_bytes, void *stream,
                               void *ev_start, void *ev_stop);
 
+/*
+ * Dense attention over packed sequences.  [Sec. 3.1, Stage 1: attention of every token of a set over every
+ * token of another (the same set, or image tokens against volume tokens and back), grouped-query heads, for
+ * batches of objects whose sets differ in length.]
+ *
+ * Sequence s owns the rows q_offsets[s] .. q_offsets[s+1] - 1 of q (its slot) and k_offsets[s] .. of k and v.
+ * The first q_lens[s] / k_lens[s] rows of a slot are its queries and keys, all of them without the lengths; so a
+ * packed batch, a batch padded to one length and a cache of keys and values with room to grow are all described
+ * alike.  With Lq queries and Lk keys, query i of a sequence stands at position i + Lk - Lq and key j at position
+ * j: queries fewer than the keys are the last of the sequence (new tokens over a cache).
+ *   S_ij = scale q_i . k_j + bias[head][bucket(j - position of i)]       (the bias where n_buckets > 0)
+ *   query i sees every key of its sequence, with `causal` those with j <= its position
+ *   out_i = sum_j softmax(S_i)_j v_j;  a query that sees no key (no keys, or causal with Lq > Lk) gives zeros.
+ * bucket(r) = number of bucket_bounds that are <= r: bucket 0 holds all distances below the first bound, the last
+ * one all from the last bound on (lsrm_rel_bucket_bounds makes the usual exact-then-logarithmic ones).
+ *
+ * Offsets that do not ascend or leave the tensors, and lengths that do not fit their slot, are cut to what does: no
+ * access leaves the tensors, but what such sequences get is unspecified.  q, k, v (and dout) of the sequences have
+ * to be finite: a masked key's infinity or NaN may reach the other queries that are worked on beside those that see
+ * it.  Rows of no sequence, and rows of a slot behind its length, may hold anything.
+ */
+typedef struct lsrm_attn_params {
+    int64_t n_q, n_k; /* rows of q (and out) and of k, v, at most 2^30                                     */
+    int32_t n_seq;    /* sequences                                                                        */
+    int32_t h_q;      /* query heads; (h_q / h_kv) * n_q at most 2^30                                     */
+    int32_t h_kv;     /* key/value heads, a divisor of h_q: query head i reads head i / (h_q / h_kv)      */
+    int32_t d;        /* head dimension: 32, 64 or 128                                                    */
+    int32_t causal;   /* 1: a query sees no key behind its own position                                   */
+    float scale;      /* softmax scale; 0 selects 1/sqrt(d)                                               */
+    const int32_t *d_q_offsets; /* DEVICE [n_seq + 1], ascending, from >= 0 to <= n_q                     */
+    const int32_t *d_k_offsets; /* DEVICE [n_seq + 1], the same for k and v; NULL: those of q (n_k = n_q)  */
+    const int32_t *d_q_lens;    /* DEVICE, nullable [n_seq]: queries in each slot                         */
+    const int32_t *d_k_lens;    /* DEVICE, nullable [n_seq]: keys in each slot; NULL with d_k_offsets NULL: those
+                                   of q, as the offsets                                                   */
+    /* {row, head} strides in elements, multiples of 8 up to 2^24 (channels are adjacent); {0, 0}: dense, [rows][heads][d].
+       dout has those of out, dq, dk and dv those of q, k and v: slices of a fused projection work as they are. */
+    int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];
+    int32_t n_buckets;            /* 0: no bias; else buckets of the bias, 1 .. 64                         */
+    const int32_t *bucket_bounds; /* HOST, read during the call, [n_buckets - 1]: strictly ascending distances at which
+                                     the next bucket begins, within +-2^20;
+                                     (h_q / h_kv) * (last - first + 2) is at most 4096                     */
+} lsrm_attn_params;
+
+/* Bytes of scratch for lsrm_attn_forward (LSRM_WS_FORWARD) or lsrm_attn_backward (LSRM_WS_BACKWARD); 0 on invalid
+ * params, and where the call needs none. */
+size_t lsrm_attn_workspace_bytes(const lsrm_attn_params *p, int which_call);
+
+/*
+ * Forward.
+ *   d_q [n_q, h_q, d], d_k, d_v [n_k, h_kv, d]  bf16, 16-byte aligned, strides as above
+ *   d_bias [h_q, n_buckets] bf16   required where n_buckets > 0, else NULL; -1e30 and below (-inf too) mask their bucket
+ *   d_out  [n_q, h_q, d] bf16  OUT: zeros in the rows of a slot behind its length; rows of no sequence are left as
+ *          they were
+ *   d_lse  [n_q, h_q] fp32  OUT, nullable: natural-log sum-exp of the scores, -inf for a query without keys (and in
+ *          a slot's rows behind its length)
+ * bf16 MFMA contractions with fp32 accumulation, probabilities rounded to bf16 between them, softmax and bias in
+ * fp32; no atomics: results are the same bit for bit from call to call.
+ */
+lsrm_status lsrm_attn_forward(const lsrm_attn_params *p, const uint16_t *d_q, const uint16_t *d_k, const uint16_t *d_v,
+                              const uint16_t *d_bias, uint16_t *d_out, float *d_lse, void *d_ws, size_t ws_bytes,
+                              void *stream);
+
+/*
+ * Backward: gradients with respect to q, k, v and the bias.
+ *   d_q, d_k, d_v, d_bias   as passed to lsrm_attn_forward;  d_out, d_lse as it wrote them
+ *   d_dout [n_q, h_q, d] bf16
+ *   d_dq, d_dk, d_dv  bf16  OUT, strides of q, k and v: a key/value head collects the gradients of all query heads
+ *          that read it; zeros in a slot's rows behind its length; rows of no sequence are left as they were
+ *   d_dbias [h_q, n_buckets] bf16  OUT, nullable: summed over all sequences in fp32 (fp64 across workgroups),
+ *          rounded once
+ * With D_i = dout_i . out_i:  dS = P (dout V^T - D),  dq = scale dS K,  dk = scale dS^T Q,  dv = P^T dout,
+ * dbias[h][b] = sum of dS over the pairs of bucket b.  P and dS are rounded to bf16 as MFMA operands (dbias sums the
+ * unrounded ones).  Every element is summed in a fixed order: results are the same bit for bit from call to call.
+ */
+lsrm_status lsrm_attn_backward(const lsrm_attn_params *p, const uint16_t *d_q, const uint16_t *d_k, const uint16_t *d_v,
+                               const uint16_t *d_bias, const uint16_t *d_out, const float *d_lse, const uint16_t *d_dout,
+                               uint16_t *d_dq, uint16_t *d_dk, uint16_t *d_dv, uint16_t *d_dbias, void *d_ws,
+                               size_t ws_bytes, void *stream);
+
+/*
+ * Bounds for lsrm_attn_params.bucket_bounds (HOST arithmetic only): a side has n_side buckets, the first n_side / 2 for the
+ * distances 0, 1, 2, ... one each, the others for geometrically growing ranges up to max_distance, the last one for
+ * everything beyond.  two_sided 0: keys at or behind the query's position by distance, those ahead of it as distance 0;
+ * n_side - 1 bounds.  two_sided 1: n_side buckets for keys at or behind, n_side - 1 for keys ahead (distance 0
+ * belongs to the former); 2 (n_side - 1) bounds.  Buckets are numbered by ascending j - position: the farthest behind is
+ * bucket 0.  n_side 2 .. 32 (two_sided) or 64, max_distance above n_side / 2 and at least n_side - 1, up to 2^20; the
+ * geometric ranges must not be empty (LSRM_ERR_UNSUPPORTED: max_distance too small for n_side).
+ */
+lsrm_status lsrm_rel_bucket_bounds(int32_t n_side, int32_t max_distance, int32_t two_sided, int32_t *bounds, int32_t *n_bounds);
+
 #ifdef __cplusplus
 }
 #endif

@@ -45,6 +45,15 @@ class lsrm_route3d_params(ctypes.Structure):
                 ("k_i2v", ctypes.c_int32), ("k_i2i", ctypes.c_int32), ("per_token", ctypes.c_int32)]
 
 
+class lsrm_attn_params(ctypes.Structure):
+    _fields_ = [("n_q", ctypes.c_int64), ("n_k", ctypes.c_int64), ("n_seq", ctypes.c_int32), ("h_q", ctypes.c_int32),
+                ("h_kv", ctypes.c_int32), ("d", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("d_q_offsets", ctypes.c_void_p), ("d_k_offsets", ctypes.c_void_p), ("d_q_lens", ctypes.c_void_p),
+                ("d_k_lens", ctypes.c_void_p), ("q_stride", ctypes.c_int64 * 2), ("k_stride", ctypes.c_int64 * 2),
+                ("v_stride", ctypes.c_int64 * 2), ("o_stride", ctypes.c_int64 * 2), ("n_buckets", ctypes.c_int32),
+                ("bucket_bounds", ctypes.POINTER(ctypes.c_int32))]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2604_05182_amd.build` "
                       "(there is no CPU fallback)")
@@ -69,6 +78,15 @@ _lib.lsrm_nsa_forward.restype = ctypes.c_int32
 _lib.lsrm_nsa_forward.argtypes = [_pp] + [_vp] * 11 + [_sz, _vp, _vp, _vp]
 _lib.lsrm_nsa_backward.restype = ctypes.c_int32
 _lib.lsrm_nsa_backward.argtypes = [_pp] + [_vp] * 14 + [_sz, _vp, _vp, _vp]
+_ap = ctypes.POINTER(lsrm_attn_params)
+_lib.lsrm_attn_workspace_bytes.restype = _sz
+_lib.lsrm_attn_workspace_bytes.argtypes = [_ap, ctypes.c_int]
+_lib.lsrm_attn_forward.restype = ctypes.c_int32
+_lib.lsrm_attn_forward.argtypes = [_ap] + [_vp] * 7 + [_sz, _vp]
+_lib.lsrm_attn_backward.restype = ctypes.c_int32
+_lib.lsrm_attn_backward.argtypes = [_ap] + [_vp] * 12 + [_sz, _vp]
+_lib.lsrm_rel_bucket_bounds.restype = ctypes.c_int32
+_lib.lsrm_rel_bucket_bounds.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp, _vp]
 
 
 def strerror(status: int) -> str:
@@ -200,3 +218,116 @@ def lsrm_nsa_backward(p, q, k, v, kc, vc, idx, gates, lse, out_branch, dout, dq,
 def alloc_workspace(p, which: int, device="cuda") -> torch.Tensor:
     n = lsrm_workspace_bytes(p, which)
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+# ---- dense attention over packed sequences ----------------------------------------------------------------------------
+def _layout(name, t, heads=None, d=None):
+    """(shape, strides) that tensors in place of `t` must have; strides of dimensions of size 1 say nothing and are made dense."""
+    if t.dim() != 3 or t.dtype != torch.bfloat16:
+        raise ValueError(f"{name}: bf16 [rows, heads, channels] expected, got {t.dtype} {tuple(t.shape)}")
+    rows, h, c = t.shape
+    if c > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}: channels have to be adjacent")
+    head = t.stride(1) if h > 1 else c
+    row = t.stride(0) if rows > 1 else h * head
+    if row <= 0 or head <= 0:
+        raise ValueError(f"{name}: expanded rows or heads are not taken, strides {t.stride()}")
+    return tuple(t.shape), (row, head)
+
+
+def _int32(name, t, n):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous int32 [{n}] on the GPU expected")
+    return t.data_ptr()
+
+
+def make_attn_params(q, k, v, q_offsets, k_offsets=None, q_lens=None, k_lens=None, causal=False, scale=0.0,
+                     bucket_bounds=None, out=None) -> lsrm_attn_params:
+    """Describes a problem by its tensors: q bf16 [n_q, h_q, d], k, v bf16 [n_k, h_kv, d] (views of a projection are fine:
+    channels adjacent, other strides multiples of 8), offsets int32 [n_seq + 1] and lengths int32 [n_seq] on the GPU (kept
+    alive by the struct), bucket_bounds a sequence of ascending ints for a bias of len + 1 buckets, or None.  The description
+    holds for other tensors of the same shapes and strides.  out: a tensor whose strides `out` and `dout` have (default dense)."""
+    p = lsrm_attn_params()
+    (n_q, h_q, d), q_st = _layout("q", q)
+    (n_k, h_kv, d_k), k_st = _layout("k", k)
+    v_shape, v_st = _layout("v", v)
+    if d_k != d or v_shape != (n_k, h_kv, d):
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {v_shape} do not fit together")
+    o_st = (h_q * d, d)
+    if out is not None:
+        o_shape, o_st = _layout("out", out)
+        if o_shape != (n_q, h_q, d):
+            raise ValueError(f"out {o_shape} expected as q {tuple(q.shape)}")
+    n_seq = q_offsets.numel() - 1
+    p.n_q, p.n_k, p.n_seq, p.h_q, p.h_kv, p.d = n_q, n_k, n_seq, h_q, h_kv, d
+    p.causal, p.scale = (1 if causal else 0), scale
+    p.d_q_offsets, p.d_k_offsets = _int32("q_offsets", q_offsets, n_seq + 1), _int32("k_offsets", k_offsets, n_seq + 1)
+    p.d_q_lens, p.d_k_lens = _int32("q_lens", q_lens, n_seq), _int32("k_lens", k_lens, n_seq)
+    p._keepalive = (q_offsets, k_offsets, q_lens, k_lens)
+    p.q_stride[:], p.k_stride[:], p.v_stride[:], p.o_stride[:] = q_st, k_st, v_st, o_st
+    p._of = {"q": ((n_q, h_q, d), q_st), "k": ((n_k, h_kv, d), k_st), "v": ((n_k, h_kv, d), v_st), "o": ((n_q, h_q, d), o_st)}
+    if bucket_bounds is not None:
+        arr = (ctypes.c_int32 * max(len(bucket_bounds), 1))(*[int(x) for x in bucket_bounds])
+        p._bounds = arr
+        p.n_buckets = len(bucket_bounds) + 1
+        p.bucket_bounds = ctypes.cast(arr, ctypes.POINTER(ctypes.c_int32))
+    return p
+
+
+def _rows(p, which, name, t):
+    """Pointer of a tensor that has to be laid out as the description says."""
+    shape, stride = p._of[which]
+    st = t.stride()
+    if (t.shape != shape or t.dtype is not torch.bfloat16 or not t.is_cuda or (shape[0] > 1 and st[0] != stride[0]) or
+            (shape[1] > 1 and st[1] != stride[1]) or st[2] != 1):
+        raise ValueError(f"{name}: bf16 {shape} with strides {stride} on the GPU expected, got {t.dtype} {tuple(t.shape)} {st} {t.device}")
+    return t.data_ptr()
+
+
+def _dense(name, t, shape, dtype):
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {dtype} {shape} on the GPU expected, got {t.dtype} {tuple(t.shape)} {t.device}")
+    return t.data_ptr()
+
+
+def lsrm_attn_workspace_bytes(p: lsrm_attn_params, which: int) -> int:
+    return int(_lib.lsrm_attn_workspace_bytes(ctypes.byref(p), which))
+
+
+def alloc_attn_workspace(p: lsrm_attn_params, which: int, device="cuda"):
+    """Scratch for lsrm_attn_forward (LSRM_WS_FORWARD) or lsrm_attn_backward (LSRM_WS_BACKWARD); None where it needs none."""
+    n = lsrm_attn_workspace_bytes(p, which)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n > 0 else None
+
+
+def lsrm_attn_forward(p, q, k, v, out, lse=None, ws=None, bias=None, stream=None):
+    """Dense attention over packed sequences; lse fp32 [n_q, h_q] or None, bias bf16 [h_q, n_buckets] where p has buckets."""
+    nbytes = ws.numel() * ws.element_size() if ws is not None else 0
+    _check(_lib.lsrm_attn_forward(ctypes.byref(p), _rows(p, "q", "q", q), _rows(p, "k", "k", k), _rows(p, "v", "v", v),
+                                  _dense("bias", bias, (p.h_q, p.n_buckets), torch.bfloat16), _rows(p, "o", "out", out),
+                                  _dense("lse", lse, (p.n_q, p.h_q), torch.float32), _ptr(ws), nbytes, _stream(stream)),
+           "lsrm_attn_forward")
+
+
+def lsrm_attn_backward(p, q, k, v, out, lse, dout, dq, dk, dv, ws=None, bias=None, dbias=None, stream=None):
+    """Gradients of lsrm_attn_forward: dq, dk, dv laid out as q, k, v; dbias as bias, or None."""
+    nbytes = ws.numel() * ws.element_size() if ws is not None else 0
+    table = (p.h_q, p.n_buckets)
+    _check(_lib.lsrm_attn_backward(ctypes.byref(p), _rows(p, "q", "q", q), _rows(p, "k", "k", k), _rows(p, "v", "v", v),
+                                   _dense("bias", bias, table, torch.bfloat16), _rows(p, "o", "out", out),
+                                   _dense("lse", lse, (p.n_q, p.h_q), torch.float32), _rows(p, "o", "dout", dout),
+                                   _rows(p, "q", "dq", dq), _rows(p, "k", "dk", dk), _rows(p, "v", "dv", dv),
+                                   _dense("dbias", dbias, table, torch.bfloat16), _ptr(ws), nbytes, _stream(stream)),
+           "lsrm_attn_backward")
+
+
+def lsrm_rel_bucket_bounds(n_side: int, max_distance: int, two_sided: bool = True) -> list:
+    """Bounds for make_attn_params: n_side buckets a side, half of them for one distance each, the others growing geometrically
+    up to max_distance (see the header)."""
+    bounds, n = (ctypes.c_int32 * 64)(), ctypes.c_int32()
+    _check(_lib.lsrm_rel_bucket_bounds(n_side, max_distance, 1 if two_sided else 0, bounds, ctypes.byref(n)), "lsrm_rel_bucket_bounds")
+    return list(bounds[:n.value])

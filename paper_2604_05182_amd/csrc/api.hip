@@ -2,7 +2,9 @@
 // meaning, layout and ownership of every argument.
 #include <vector>
 
-#include "lsrm_internal.h"
+#include <cmath>
+
+#include "attn_internal.h"
 
 namespace lsrm {
 
@@ -71,6 +73,68 @@ static lsrm_status make_segments(const lsrm_nsa_params *p, const Shape &s, std::
         seg->push_back(o);
     }
     if (seg->back() != s.n) return LSRM_ERR_INVALID_ARG;
+    return LSRM_OK;
+}
+
+// {0, 0} or multiples of 8 that a 32-bit offset within a tile of rows can hold
+static bool strides_of(const int64_t (&given)[2], int heads, int d, int64_t (&out)[2]) {
+    if (given[0] == 0 && given[1] == 0) {
+        out[0] = (int64_t)heads * d;
+        out[1] = d;
+    } else {
+        out[0] = given[0];
+        out[1] = given[1];
+    }
+    for (int64_t x : out)
+        if (x <= 0 || x % 8 != 0 || x > (int64_t)1 << 24) return false;
+    return true;
+}
+
+lsrm_status make_attn_args(const lsrm_attn_params *p, AttnArgs *a) {
+    if (p == nullptr) return LSRM_ERR_INVALID_ARG;
+    *a = AttnArgs{};
+    if (p->n_q < 0 || p->n_k < 0 || p->n_seq < 0 || p->h_q <= 0 || p->h_kv <= 0 || p->d <= 0) return LSRM_ERR_INVALID_ARG;
+    if (p->h_q % p->h_kv != 0 || (p->causal != 0 && p->causal != 1)) return LSRM_ERR_INVALID_ARG;
+    if (!(p->scale >= 0.0f) || __builtin_isinf(p->scale)) return LSRM_ERR_INVALID_ARG;
+    if (p->n_seq > 0 && p->d_q_offsets == nullptr) return LSRM_ERR_INVALID_ARG;
+    if (p->d_k_offsets == nullptr && p->n_k != p->n_q) return LSRM_ERR_INVALID_ARG;
+    if (p->n_buckets < 0 || (p->n_buckets > 1 && p->bucket_bounds == nullptr)) return LSRM_ERR_INVALID_ARG;
+    if (p->d != 32 && p->d != 64 && p->d != 128) return LSRM_ERR_UNSUPPORTED;
+    const int64_t most = (int64_t)1 << 30;
+    if (p->n_q > most || p->n_k > most || p->n_q * (p->h_q / p->h_kv) > most) return LSRM_ERR_UNSUPPORTED;
+    a->group = p->h_q / p->h_kv;
+    // workgroups of 256 threads that a launch can have
+    const int64_t wgs = (int64_t)1 << 23, rows = p->n_q * a->group;
+    if ((rows / 32 + p->n_seq) * p->h_kv > wgs || (p->n_q / 128 + p->n_seq) * p->h_q > wgs || (p->n_k / 128 + p->n_seq) * p->h_kv > wgs)
+        return LSRM_ERR_UNSUPPORTED;
+    if (!strides_of(p->q_stride, p->h_q, p->d, a->qs) || !strides_of(p->k_stride, p->h_kv, p->d, a->ks) ||
+        !strides_of(p->v_stride, p->h_kv, p->d, a->vs) || !strides_of(p->o_stride, p->h_q, p->d, a->os))
+        return LSRM_ERR_INVALID_ARG;
+    a->n_q = (int)p->n_q;
+    a->n_k = (int)p->n_k;
+    a->n_seq = p->n_seq;
+    a->h_q = p->h_q;
+    a->h_kv = p->h_kv;
+    a->causal = p->causal;
+    a->q_off = p->d_q_offsets;
+    a->q_len = p->d_q_lens;
+    a->k_off = p->d_k_offsets != nullptr ? p->d_k_offsets : p->d_q_offsets;
+    a->k_len = p->d_k_offsets == nullptr && p->d_k_lens == nullptr ? p->d_q_lens : p->d_k_lens;
+    a->scale = p->scale > 0.0f ? p->scale : 1.0f / __builtin_sqrtf((float)p->d);
+    a->sl2 = a->scale * kLog2e;
+    if (__builtin_isinf(a->sl2)) return LSRM_ERR_INVALID_ARG;
+    a->n_buckets = p->n_buckets;
+    if (p->n_buckets > 0) {
+        if (p->n_buckets > kMaxBuckets) return LSRM_ERR_UNSUPPORTED;
+        for (int i = 0; i < p->n_buckets - 1; ++i) {
+            a->bounds[i] = p->bucket_bounds[i];
+            if (a->bounds[i] > 1 << 20 || a->bounds[i] < -(1 << 20)) return LSRM_ERR_UNSUPPORTED;
+            if (i > 0 && a->bounds[i] <= a->bounds[i - 1]) return LSRM_ERR_INVALID_ARG;
+        }
+        a->b0 = p->n_buckets > 1 ? a->bounds[0] : 0;
+        a->tab = p->n_buckets > 1 ? a->bounds[p->n_buckets - 2] - a->b0 + 2 : 2;
+        if ((int64_t)a->group * a->tab > kMaxBiasEntries) return LSRM_ERR_UNSUPPORTED;
+    }
     return LSRM_OK;
 }
 
@@ -221,6 +285,94 @@ lsrm_status lsrm_nsa_backward(const lsrm_nsa_params *p, const uint16_t *d_q, con
     return launch_backward(s, seg.data(), (int)seg.size() - 1, d_q, d_k, d_v, d_kc, d_vc, d_idx, d_gates, d_lse,
                            d_out_branch, d_dout, d_dq, d_dk, d_dv, d_ws, static_cast<hipStream_t>(stream),
                            static_cast<hipEvent_t>(ev_start), static_cast<hipEvent_t>(ev_stop));
+}
+
+size_t lsrm_attn_workspace_bytes(const lsrm_attn_params *p, int which_call) {
+    AttnArgs a;
+    if (make_attn_args(p, &a) != LSRM_OK) return 0;
+    switch (which_call) {
+        case LSRM_WS_FORWARD: return attn_forward_ws_bytes(a, p->d);
+        case LSRM_WS_BACKWARD: return attn_backward_ws_bytes(a, p->d);
+        default: return 0;
+    }
+}
+
+lsrm_status lsrm_attn_forward(const lsrm_attn_params *p, const uint16_t *d_q, const uint16_t *d_k, const uint16_t *d_v,
+                              const uint16_t *d_bias, uint16_t *d_out, float *d_lse, void *d_ws, size_t ws_bytes, void *stream) {
+    AttnArgs a;
+    lsrm_status rc = make_attn_args(p, &a);
+    if (rc != LSRM_OK) return rc;
+    if ((a.n_buckets > 0) != (d_bias != nullptr)) return LSRM_ERR_INVALID_ARG;
+    if (a.n_seq == 0 || a.n_q == 0) return LSRM_OK;
+    if (d_q == nullptr || d_out == nullptr || (a.n_k > 0 && (d_k == nullptr || d_v == nullptr))) return LSRM_ERR_INVALID_ARG;
+    if (!aligned(d_q, 16) || !aligned(d_k, 16) || !aligned(d_v, 16) || !aligned(d_out, 16) || !aligned(d_bias, 2) || !aligned(d_lse, 4))
+        return LSRM_ERR_INVALID_ARG;
+    const size_t need = attn_forward_ws_bytes(a, p->d);
+    if (need > 0 && (d_ws == nullptr || !aligned(d_ws, 256) || ws_bytes < need)) return LSRM_ERR_WORKSPACE;
+    a.q = d_q;
+    a.k = d_k;
+    a.v = d_v;
+    a.bias = d_bias;
+    a.out = d_out;
+    a.lse = d_lse;
+    return launch_attn_forward(a, p->d, d_ws, static_cast<hipStream_t>(stream));
+}
+
+lsrm_status lsrm_attn_backward(const lsrm_attn_params *p, const uint16_t *d_q, const uint16_t *d_k, const uint16_t *d_v,
+                               const uint16_t *d_bias, const uint16_t *d_out, const float *d_lse, const uint16_t *d_dout, uint16_t *d_dq,
+                               uint16_t *d_dk, uint16_t *d_dv, uint16_t *d_dbias, void *d_ws, size_t ws_bytes, void *stream) {
+    AttnArgs a;
+    lsrm_status rc = make_attn_args(p, &a);
+    if (rc != LSRM_OK) return rc;
+    if ((a.n_buckets > 0) != (d_bias != nullptr) || (d_dbias != nullptr && a.n_buckets == 0)) return LSRM_ERR_INVALID_ARG;
+    if (a.n_seq > 0) {
+        const void *of_q[] = {d_q, d_out, d_lse, d_dout, d_dq}, *of_k[] = {d_k, d_v, d_dk, d_dv};
+        for (const void *x : of_q)
+            if ((a.n_q > 0 && x == nullptr) || !aligned(x, x == d_lse ? 4 : 16)) return LSRM_ERR_INVALID_ARG;
+        for (const void *x : of_k)
+            if ((a.n_k > 0 && x == nullptr) || !aligned(x, 16)) return LSRM_ERR_INVALID_ARG;
+    }
+    if (!aligned(d_bias, 2) || !aligned(d_dbias, 2)) return LSRM_ERR_INVALID_ARG;
+    const size_t need = attn_backward_ws_bytes(a, p->d);
+    if (need > 0 && (d_ws == nullptr || !aligned(d_ws, 256) || ws_bytes < need)) return LSRM_ERR_WORKSPACE;
+    a.q = d_q;
+    a.k = d_k;
+    a.v = d_v;
+    a.bias = d_bias;
+    a.o = d_out;
+    a.lse_in = d_lse;
+    a.dout = d_dout;
+    a.dq = d_dq;
+    a.dk = d_dk;
+    a.dv = d_dv;
+    a.dbias = d_dbias;
+    return launch_attn_backward(a, p->d, d_ws, static_cast<hipStream_t>(stream));
+}
+
+lsrm_status lsrm_rel_bucket_bounds(int32_t n_side, int32_t max_distance, int32_t two_sided, int32_t *bounds, int32_t *n_bounds) {
+    if (bounds == nullptr || n_bounds == nullptr || n_side < 2 || max_distance < 1 || (two_sided != 0 && two_sided != 1))
+        return LSRM_ERR_INVALID_ARG;
+    if (n_side > (two_sided ? kMaxBuckets / 2 : kMaxBuckets) || max_distance > 1 << 20) return LSRM_ERR_UNSUPPORTED;
+    const int single = n_side / 2;  // distances 0 .. single - 1 have a bucket each
+    int32_t start[kMaxBuckets];     // start[b]: smallest distance of bucket b
+    for (int b = 0; b < n_side; ++b) {
+        if (b <= single) {
+            start[b] = b;
+        } else {
+            // the smallest distance with  ln(distance / single) / ln(max_distance / single) (n_side - single) >= b - single;  a distance
+            // that the border meets exactly belongs to the higher bucket, whichever way the logarithms were rounded
+            const double x = single * std::pow((double)max_distance / single, (double)(b - single) / (n_side - single));
+            start[b] = (int32_t)std::ceil(x * (1.0 - 1e-9));
+        }
+        if (b > 0 && start[b] <= start[b - 1]) return LSRM_ERR_UNSUPPORTED;
+    }
+    // behind the query: j - position = -distance; a bucket of distances start[b] .. start[b + 1] - 1 begins at -(start[b + 1] - 1)
+    int n = 0;
+    for (int b = n_side - 2; b >= 0; --b) bounds[n++] = 1 - start[b + 1];
+    if (two_sided)
+        for (int b = 1; b < n_side; ++b) bounds[n++] = start[b];
+    *n_bounds = n;
+    return LSRM_OK;
 }
 
 }  // extern "C"

@@ -1,0 +1,503 @@
+// Dense attention over packed sequences, backward, on gfx950.
+//
+// With P = softmax probabilities recomputed from the saved log-sum-exp, D_i = dout_i . out_i, dP = dout V^T:
+//     dV = P^T dout      dS = P o (dP - D)      dQ = scale dS K      dK = scale dS^T Q      dB[b] = sum of dS over bucket b
+// Two passes that each own their output rows (no atomics between workgroups, one order of sums):
+//   attn_dq_kernel   128 query rows to a workgroup, one query row per lane (S^T = K Q^T), walks the keys; works out D for itself
+//                    and leaves it, with the log-sum-exp, for the other pass; sums dS by distance.
+//   attn_dkv_kernel  128 keys of a key/value head to a workgroup, one key per lane (S = Q K^T), walks the queries of the heads that
+//                    read them.
+#include "attn_internal.h"
+
+#include <algorithm>
+
+namespace lsrm {
+
+namespace {
+
+constexpr int kStage = 64;  // keys per stage of the dQ pass
+template <int D>
+constexpr int kDqLds = 2 * kStage * 2 * AttnGeo<D>::ROW;
+template <int D>
+constexpr int kDkvSlot = 2 * AttnGeo<D>::TILE + 256;  // 32 rows of q, of dout, and their entries of aux
+template <int D>
+constexpr int kDkvLds = 4 * 32 * AttnGeo<D>::OUT_ROW > 2 * kDkvSlot<D> ? 4 * 32 * AttnGeo<D>::OUT_ROW : 2 * kDkvSlot<D>;
+
+__device__ __forceinline__ void lds_add(float *at, float x) {
+    asm volatile("ds_add_f32 %0, %1" ::"v"((uint32_t)(uintptr_t)at), "v"(x) : "memory");
+}
+
+template <int D, bool BIAS>
+__global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
+    using G = AttnGeo<D>;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
+    const int head_kv = blockIdx.x % a.h_kv, place = blockIdx.x / a.h_kv;
+    const int part = place % a.parts;
+    const int slot = a.causal ? a.n_slots - 1 - place / a.parts : place / a.parts;
+    const int seq = find_sequence(a.q_off, a.n_q, a.n_seq, a.group, 128, slot);
+    const Sequence s = load_sequence(a, seq);
+    const int v_wg = (slot - tile_slot(a.q_off, a.n_q, a.group, 128, seq)) * 128, slot_rows = s.q_slot * a.group;
+    const int n_rows = s.n_q * a.group;
+    if (v_wg < 0 || v_wg >= slot_rows) {
+        if (BIAS && a.part_bias != nullptr)
+            for (int i = threadIdx.x; i < a.group * a.n_buckets; i += 256)
+                a.part_bias[((int64_t)slot * a.h_q + head_kv * a.group) * a.n_buckets + i] = 0.f;
+        return;
+    }
+    auto seen = [&](int pos) { return a.causal ? min(max(pos + 1, 0), s.n_k) : s.n_k; };
+    const int keys = v_wg < n_rows ? seen(min(v_wg + 127, n_rows - 1) / a.group + s.shift) : 0;
+    const int st_all = (keys + kStage - 1) / kStage, st_per = (st_all + a.parts - 1) / a.parts;
+    const int st_begin = part * st_per, st_end = min(st_begin + st_per, st_all);
+    const char *kb = reinterpret_cast<const char *>(a.k + s.k0 * a.ks[0] + head_kv * a.ks[1]);
+    const char *vb = reinterpret_cast<const char *>(a.v + s.k0 * a.vs[0] + head_kv * a.vs[1]);
+    const uint32_t k_row = (uint32_t)a.ks[0] * 2, v_row = (uint32_t)a.vs[0] * 2;
+    const CopyLane<D> c(lane);
+    auto copy_stage = [&](int st) {
+        char *at = lds + ((st - st_begin) & 1) * (2 * kStage * G::ROW);
+        const int j0 = st * kStage;
+        copy_rows<D, kStage, 4>(kb + (uint64_t)j0 * k_row, k_row, keys - j0, at, wave, c);
+        copy_rows<D, kStage, 4>(vb + (uint64_t)j0 * v_row, v_row, keys - j0, at + kStage * G::ROW, wave, c);
+    };
+    if (st_begin < st_end) copy_stage(st_begin);
+    // bias: expanded, then the sums of dS by distance of each wavefront, then what a workgroup ends with
+    float *tab = reinterpret_cast<float *>(lds + kDqLds<D>);
+    const int n_tab = a.group * a.tab;
+    float *near = tab + (1 + wave) * n_tab, *far = tab + 5 * n_tab;
+    if (BIAS) {
+        expand_bias(a, head_kv, tab, 256);
+        for (int i = threadIdx.x; i < 4 * n_tab; i += 256) tab[n_tab + i] = 0.f;
+    }
+
+    const int v0 = v_wg + wave * 32, v = v0 + (lane & 31);
+    const bool live = v < n_rows;
+    const int last = max(min(v0 + 31, n_rows - 1), 0), vc = min(v, last);  // rows behind the last one do its work again, with P = 0
+    const int tok = (unsigned)vc / (unsigned)a.group, g = vc - tok * a.group, head = head_kv * a.group + g;
+    const int pos = tok + s.shift, pos_min = v0 / a.group + s.shift, pos_max = last / a.group + s.shift;
+    const int lim = seen(pos), lim_min = seen(pos_min), lim_max = v0 < n_rows ? seen(pos_max) : 0;
+    bf16x8 q[G::NS], dout[G::NS];
+    float off = __builtin_inff(), delta = 0.f;
+    if (v0 < n_rows) {
+        const uint16_t *qp = a.q + (s.q0 + tok) * a.qs[0] + head * a.qs[1] + 8 * hh;
+        const int64_t o_at = (s.q0 + tok) * a.os[0] + head * a.os[1] + 8 * hh;
+#pragma unroll
+        for (int ks = 0; ks < G::NS; ++ks) {
+            q[ks] = *reinterpret_cast<const bf16x8 *>(qp + 16 * ks);
+            dout[ks] = *reinterpret_cast<const bf16x8 *>(a.dout + o_at + 16 * ks);
+            const bf16x8 o = *reinterpret_cast<const bf16x8 *>(a.o + o_at + 16 * ks);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) delta += (float)dout[ks][i] * (float)o[i];
+        }
+        delta = half_sum(delta);
+        const float lse = a.lse_in[(int64_t)(s.q0 + tok) * a.h_q + head];
+        if (live && lse != -__builtin_inff()) off = lse * kLog2e;
+        if (live && hh == 0 && part == 0) a.aux[(int64_t)head * a.n_q + s.q0 + tok] = make_float2(off, -delta);
+    } else {
+#pragma unroll
+        for (int ks = 0; ks < G::NS; ++ks) q[ks] = dout[ks] = bf16x8{};
+    }
+    f32x16 dq[G::ND];
+#pragma unroll
+    for (int dt = 0; dt < G::ND; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dq[dt][i] = 0.f;
+    // of this lane's row: sums of dS over all keys, and of dS and P over those before the first and behind the last bound
+    float sum_all = 0.f, sum_lo = 0.f, sum_hi = 0.f, p_lo = 0.f, p_hi = 0.f;
+    const int b_last = a.b0 + a.tab - 2;
+    const float *tab_g = tab + g * a.tab;
+    const TileLane<D> t(lane);
+    for (int st = st_begin; st < st_end; ++st) {
+        wait_copies<0>();
+        wg_barrier();
+        if (st + 1 < st_end) copy_stage(st + 1);
+        const char *at = lds + ((st - st_begin) & 1) * (2 * kStage * G::ROW);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int j0 = st * kStage + 32 * h;
+            if (j0 >= lim_max) continue;
+            const char *kt = at + h * G::TILE, *vt = at + (kStage + 32 * h) * G::ROW;
+            f32x16 x, dp;
+            mfma_rows<D>(x, kt, t, q);
+            mfma_rows<D>(dp, vt, t, dout);
+            const bool behind = BIAS && j0 + 31 - pos_min < a.b0, ahead = BIAS && j0 - pos_max >= b_last;
+            const int x0 = j0 - pos - a.b0 + 1;
+            if (BIAS) {
+                if (behind || ahead) {
+                    const float b = tab_g[ahead ? a.tab - 1 : 0];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = x[i] * a.sl2 + b;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = x[i] * a.sl2 + tab_g[min(max(x0 + acc_row(i, hh), 0), a.tab - 1)];
+                }
+            }
+            if (j0 + 32 > lim_min) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (j0 + acc_row(i, hh) >= lim) x[i] = -__builtin_inff();
+            }
+            float p_sum = 0.f, ds_sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float p = __builtin_amdgcn_exp2f(BIAS ? x[i] - off : x[i] * a.sl2 - off);
+                dp[i] = p * (dp[i] - delta);
+                if (BIAS) {
+                    x[i] = p;
+                    p_sum += p;
+                    ds_sum += dp[i];
+                }
+            }
+            if (BIAS) {
+                sum_all += ds_sum;
+                if (behind) {
+                    sum_lo += ds_sum;
+                    p_lo += p_sum;
+                } else if (ahead) {
+                    sum_hi += ds_sum;
+                    p_hi += p_sum;
+                } else {
+                    // At the same time only lanes of one half: those of a head then add to different distances, so that the order of every
+                    // sum is that of the program (the LDS operations of a wavefront execute in order).
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int at_x = x0 + acc_row(i, hh);
+                        if (at_x <= 0) {
+                            sum_lo += dp[i];
+                            p_lo += x[i];
+                        } else if (at_x >= a.tab - 1) {
+                            sum_hi += dp[i];
+                            p_hi += x[i];
+                        } else {
+                            float *to = near + g * a.tab + at_x;
+                            if (hh == 0) lds_add(to, dp[i]);
+                            if (hh == 1) lds_add(to, dp[i]);
+                        }
+                    }
+                }
+            }
+            BFrag b[2];
+            to_b_operand(dp, b);
+            mfma_transposed<D>(dq, kt, t, b);
+        }
+    }
+    wait_copies<0>();
+    wg_barrier();
+    mfma_settle();
+    if (a.parts == 1) {
+        store_query_rows<D>(a, s, head_kv, v0, slot_rows, dq, a.scale, live, lds + wave * 32 * G::OUT_ROW, a.dq, a.qs, lane);
+    } else if (v < slot_rows) {
+        const int to_tok = (unsigned)v / (unsigned)a.group, to_head = head_kv * a.group + v - to_tok * a.group;
+        float *to = a.part_q + (((int64_t)part * a.n_q + s.q0 + to_tok) * a.h_q + to_head) * D + 4 * hh;
+#pragma unroll
+        for (int dt = 0; dt < G::ND; ++dt)
+#pragma unroll
+            for (int gq = 0; gq < 4; ++gq) {
+                const float z = live ? a.scale : 0.f;
+                *reinterpret_cast<f32x4 *>(to + 32 * dt + 8 * gq) =
+                    f32x4{dq[dt][4 * gq] * z, dq[dt][4 * gq + 1] * z, dq[dt][4 * gq + 2] * z, dq[dt][4 * gq + 3] * z};
+            }
+    }
+    if (BIAS && a.part_bias != nullptr) {
+        // D comes from outputs that were rounded: it is off by the sum of dS over all keys, which belongs to be zero.  The far
+        // buckets, sums over many keys that nearly cancel, are put right by it.
+        const float miss = half_sum(sum_all);
+        const float lo = half_sum(sum_lo) - miss * half_sum(p_lo), hi = half_sum(sum_hi) - miss * half_sum(p_hi);
+        if (hh == 0) {
+            far[wave * 64 + lane] = live ? lo : 0.f;
+            far[wave * 64 + 32 + lane] = live ? hi : 0.f;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wg_barrier();
+        for (int i = threadIdx.x; i < a.group * a.n_buckets; i += 256) {
+            const int gi = i / a.n_buckets, b = i % a.n_buckets;
+            float sum = 0.f;
+            if (b > 0 && b < a.n_buckets - 1)
+                for (int w = 0; w < 4; ++w)
+                    for (int z = a.bounds[b - 1] - a.b0 + 1; z < a.bounds[b] - a.b0 + 1; ++z) sum += tab[(1 + w) * n_tab + gi * a.tab + z];
+            if (b == 0 || b == a.n_buckets - 1) {
+                // rows of this head: (row % group) == gi
+                for (int z = (gi + a.group - v_wg % a.group) % a.group; z < 128; z += a.group) {
+                    const float *f = far + (z / 32) * 64 + z % 32;
+                    if (b == 0) sum += f[0];
+                    if (b == a.n_buckets - 1) sum += f[32];
+                }
+            }
+            a.part_bias[((int64_t)slot * a.h_q + head_kv * a.group) * a.n_buckets + i] = sum;
+        }
+    }
+}
+
+template <int D, bool BIAS>
+__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attn_dkv_kernel(AttnArgs a) {
+    using G = AttnGeo<D>;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
+    const int head_kv = blockIdx.x % a.h_kv, place = blockIdx.x / a.h_kv;
+    const int part = place % a.parts, slot = place / a.parts;
+    const int seq = find_sequence(a.k_off, a.n_k, a.n_seq, 1, 128, slot);
+    const Sequence s = load_sequence(a, seq);
+    const int j_wg = (slot - tile_slot(a.k_off, a.n_k, 1, 128, seq)) * 128;
+    if (j_wg < 0 || j_wg >= s.k_slot) return;
+    const int j0 = j_wg + wave * 32, j = j0 + (lane & 31);
+    const bool live = j < s.n_k;
+    // query tiles of 32: those of a head from the first that sees a key of this workgroup on, head after head
+    const int n_t = (s.n_q + 31) / 32, t0 = a.causal ? min(max(j_wg - s.shift, 0) / 32, n_t) : 0;
+    const int n_all = j_wg < s.n_k ? a.group * (n_t - t0) : 0, per = (n_all + a.parts - 1) / a.parts;
+    const int i_begin = part * per, i_end = min(i_begin + per, n_all);
+    bf16x8 kf[G::NS], vf[G::NS];
+    f32x16 dk[G::ND], dv[G::ND];
+#pragma unroll
+    for (int dt = 0; dt < G::ND; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dk[dt][i] = dv[dt][i] = 0.f;
+    if (i_begin < i_end) {
+        const uint32_t q_row = (uint32_t)a.qs[0] * 2, o_row = (uint32_t)a.os[0] * 2;
+        const CopyLane<D> c(lane);
+        auto copy_tile = [&](int i, int g, int qt) {
+            char *at = lds + ((i - i_begin) & 1) * kDkvSlot<D>;
+            const int head = head_kv * a.group + g, avail = s.n_q - 32 * qt;
+            const int64_t row = s.q0 + 32 * qt;
+            copy_rows<D, 32, 4 < G::COPIES ? 4 : G::COPIES>(reinterpret_cast<const char *>(a.q + row * a.qs[0] + head * a.qs[1]), q_row, avail, at,
+                                                            wave % G::COPIES, c);
+            copy_rows<D, 32, 4 < G::COPIES ? 4 : G::COPIES>(reinterpret_cast<const char *>(a.dout + row * a.os[0] + head * a.os[1]), o_row, avail,
+                                                            at + G::TILE, wave % G::COPIES, c);
+            if (wave == 0)
+                copy_256_to_lds(a.aux + (int64_t)head * a.n_q + row, min(lane & 31, avail - 1) * 8 + hh * 4, at + 2 * G::TILE);
+        };
+        int g = i_begin / (n_t - t0), qt = t0 + i_begin % (n_t - t0);
+        copy_tile(i_begin, g, qt);
+        float *tab = reinterpret_cast<float *>(lds + kDkvLds<D>);
+        if (BIAS) expand_bias(a, head_kv, tab, 256);
+        const int jc = min(j, s.n_k - 1);
+        const uint16_t *kp = a.k + (s.k0 + jc) * a.ks[0] + head_kv * a.ks[1] + 8 * hh;
+        const uint16_t *vp = a.v + (s.k0 + jc) * a.vs[0] + head_kv * a.vs[1] + 8 * hh;
+#pragma unroll
+        for (int ks = 0; ks < G::NS; ++ks) {
+            kf[ks] = *reinterpret_cast<const bf16x8 *>(kp + 16 * ks);
+            vf[ks] = *reinterpret_cast<const bf16x8 *>(vp + 16 * ks);
+        }
+        const TileLane<D> t(lane);
+        const int b_last = a.b0 + a.tab - 2;
+        for (int i = i_begin; i < i_end; ++i) {
+            wait_copies<0>();
+            wg_barrier();
+            int g_next = g, qt_next = qt + 1;
+            if (qt_next == n_t) {
+                qt_next = t0;
+                ++g_next;
+            }
+            if (i + 1 < i_end) copy_tile(i + 1, g_next, qt_next);
+            const int p0 = 32 * qt + s.shift;  // position of the tile's first query
+            if (j0 < s.n_k && !(a.causal && p0 + 31 < j0)) {
+                const char *at = lds + ((i - i_begin) & 1) * kDkvSlot<D>;
+                const float *aux = reinterpret_cast<const float *>(at + 2 * G::TILE) + 8 * hh;
+                f32x16 x, dp;
+                mfma_rows<D>(x, at, t, kf);
+                mfma_rows<D>(dp, at + G::TILE, t, vf);
+                if (BIAS) {
+                    const float *tab_g = tab + g * a.tab;
+                    if (j0 + 31 - p0 < a.b0 || j0 - p0 - 31 >= b_last) {
+                        const float b = tab_g[j0 - p0 - 31 >= b_last ? a.tab - 1 : 0];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = x[e] * a.sl2 + b;
+                    } else {
+                        const int x0 = j - p0 - a.b0 + 1;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = x[e] * a.sl2 + tab_g[min(max(x0 - acc_row(e, hh), 0), a.tab - 1)];
+                    }
+                }
+                if (32 * qt + 32 > s.n_q || (a.causal && j0 + 31 > p0)) {
+                    // rows of the tile that are queries and see this lane's key
+                    const int from = a.causal ? j - p0 : 0, to = s.n_q - 32 * qt;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int row = acc_row(e, hh);
+                        if (row < from || row >= to) x[e] = -__builtin_inff();
+                    }
+                }
+                f32x16 p;
+#pragma unroll
+                for (int e4 = 0; e4 < 16; e4 += 4) {
+                    const f32x4 off = *reinterpret_cast<const f32x4 *>(aux + 16 * (e4 / 8) + e4 % 8);
+                    const f32x4 nd = *reinterpret_cast<const f32x4 *>(aux + 32 + 16 * (e4 / 8) + e4 % 8);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[e4 + e] = __builtin_amdgcn_exp2f(BIAS ? x[e4 + e] - off[e] : x[e4 + e] * a.sl2 - off[e]);
+                        dp[e4 + e] = p[e4 + e] * (dp[e4 + e] + nd[e]);
+                    }
+                }
+                BFrag b[2];
+                to_b_operand(p, b);
+                mfma_transposed<D>(dv, at + G::TILE, t, b);
+                to_b_operand(dp, b);
+                mfma_transposed<D>(dk, at, t, b);
+            }
+            g = g_next;
+            qt = qt_next;
+        }
+    }
+    wait_copies<0>();
+    wg_barrier();
+    mfma_settle();
+    if (a.parts == 1) {
+        // (a key/value head's rows: the same as query rows of a group of one)
+        char *stage = lds + wave * 32 * G::OUT_ROW;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const f32x16(&x)[G::ND] = which == 0 ? dk : dv;
+            const float mul = which == 0 ? a.scale : 1.0f;
+#pragma unroll
+            for (int dt = 0; dt < G::ND; ++dt)
+#pragma unroll
+                for (int gq = 0; gq < 4; ++gq) {
+                    uint2 w;
+                    w.x = live ? pack_bf16(x[dt][4 * gq] * mul, x[dt][4 * gq + 1] * mul) : 0;
+                    w.y = live ? pack_bf16(x[dt][4 * gq + 2] * mul, x[dt][4 * gq + 3] * mul) : 0;
+                    *reinterpret_cast<uint2 *>(stage + (lane & 31) * G::OUT_ROW + (32 * dt + 8 * gq + 4 * hh) * 2) = w;
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            constexpr int CH = D / 8, RPP = 64 / CH;
+            uint16_t *dst = which == 0 ? a.dk + s.k0 * a.ks[0] + head_kv * a.ks[1] : a.dv + s.k0 * a.vs[0] + head_kv * a.vs[1];
+            const int64_t step = which == 0 ? a.ks[0] : a.vs[0];
+#pragma unroll
+            for (int it = 0; it < 32 / RPP; ++it) {
+                const int rr = it * RPP + lane / CH;
+                const uint4 w = *reinterpret_cast<const uint4 *>(stage + rr * G::OUT_ROW + (lane % CH) * 16);
+                if (j0 + rr < s.k_slot) *reinterpret_cast<uint4 *>(dst + (j0 + rr) * step + 8 * (lane % CH)) = w;
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+    } else if (j < s.k_slot) {
+        const int64_t at = (((int64_t)part * a.n_k + s.k0 + j) * a.h_kv + head_kv) * D + 4 * hh;
+        const float z = live ? 1.0f : 0.f, zk = z * a.scale;
+#pragma unroll
+        for (int dt = 0; dt < G::ND; ++dt)
+#pragma unroll
+            for (int gq = 0; gq < 4; ++gq) {
+                *reinterpret_cast<f32x4 *>(a.part_k + at + 32 * dt + 8 * gq) =
+                    f32x4{dk[dt][4 * gq] * zk, dk[dt][4 * gq + 1] * zk, dk[dt][4 * gq + 2] * zk, dk[dt][4 * gq + 3] * zk};
+                *reinterpret_cast<f32x4 *>(a.part_v + at + 32 * dt + 8 * gq) =
+                    f32x4{dv[dt][4 * gq] * z, dv[dt][4 * gq + 1] * z, dv[dt][4 * gq + 2] * z, dv[dt][4 * gq + 3] * z};
+            }
+    }
+}
+
+// Parts of dQ (Q) or of dK and dV, added in order.  A workgroup: up to 128 rows of a sequence's slot, one head.
+template <int D, bool Q>
+__global__ __launch_bounds__(256) void attn_sum_parts(AttnArgs a) {
+    const int heads = Q ? a.h_q : a.h_kv, n = Q ? a.n_q : a.n_k;
+    const int32_t *offs = Q ? a.q_off : a.k_off;
+    const int head = blockIdx.x % heads, slot = blockIdx.x / heads;
+    const int seq = find_sequence(offs, n, a.n_seq, 1, 128, slot);
+    const Sequence s = load_sequence(a, seq);
+    const int first = (slot - tile_slot(offs, n, 1, 128, seq)) * 128, rows = Q ? s.q_slot : s.k_slot, row0 = Q ? s.q0 : s.k0;
+    if (first < 0 || first >= rows) return;
+    constexpr int CH = D / 8;
+    const int64_t step = (int64_t)n * heads * D;
+    for (int which = 0; which < (Q ? 1 : 2); ++which) {
+        const float *from = Q ? a.part_q : which == 0 ? a.part_k : a.part_v;
+        uint16_t *dst = Q ? a.dq : which == 0 ? a.dk : a.dv;
+        const int64_t *stride = Q ? a.qs : which == 0 ? a.ks : a.vs;
+        for (int i = threadIdx.x; i < 128 * CH; i += 256) {
+            const int r = first + i / CH, ch = i % CH;
+            if (r >= rows) break;
+            const float *at = from + ((int64_t)(row0 + r) * heads + head) * D + 8 * ch;
+            f32x4 x = *reinterpret_cast<const f32x4 *>(at), y = *reinterpret_cast<const f32x4 *>(at + 4);
+            for (int p = 1; p < a.parts; ++p) {
+                x += *reinterpret_cast<const f32x4 *>(at + p * step);
+                y += *reinterpret_cast<const f32x4 *>(at + p * step + 4);
+            }
+            *reinterpret_cast<uint4 *>(dst + (int64_t)(row0 + r) * stride[0] + head * stride[1] + 8 * ch) =
+                make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+        }
+    }
+}
+
+// The bias' gradient: what the workgroups of a head left, added in order (in 64 bits).
+__global__ __launch_bounds__(256) void attn_sum_bias(AttnArgs a) {
+    __shared__ double sums[4][kMaxBuckets];
+    const int head = blockIdx.x, b = threadIdx.x % 64, way = threadIdx.x / 64;
+    double x = 0.;
+    if (b < a.n_buckets)
+        for (int i = way; i < a.n_slots; i += 4) x += a.part_bias[((int64_t)i * a.h_q + head) * a.n_buckets + b];
+    sums[way][b] = x;
+    __syncthreads();
+    if (way == 0 && b < a.n_buckets) {
+        const __bf16 y = (__bf16)(float)(sums[0][b] + sums[1][b] + sums[2][b] + sums[3][b]);
+        a.dbias[head * a.n_buckets + b] = *reinterpret_cast<const uint16_t *>(&y);
+    }
+}
+
+// Where there are few workgroups, walks are cut into parts, of which fp32 sums are added up afterwards.
+struct WsLayout {
+    int q_slots, k_slots, q_parts, k_parts;
+    size_t aux, part_q, part_k, part_v, part_bias, total;
+};
+WsLayout layout(const AttnArgs &a, int d) {
+    WsLayout w;
+    const int64_t rows = (int64_t)a.n_q * a.group;
+    w.q_slots = (int)(rows / 128 + a.n_seq);
+    w.k_slots = a.n_k / 128 + a.n_seq;
+    auto parts = [&](int64_t wgs, int64_t walk) {  // walk: tiles of 32 that an average workgroup walks
+        return (int)std::min<int64_t>(std::max<int64_t>(512 / std::max<int64_t>(wgs, 1), 1), std::min<int64_t>(std::max<int64_t>(walk / 8, 1), 16));
+    };
+    w.q_parts = a.n_buckets > 0 ? 1 : parts((rows / 128 + 1) * a.h_kv, (int64_t)a.n_k / a.n_seq / 32);
+    w.k_parts = parts(((int64_t)a.n_k / 128 + 1) * a.h_kv, rows / a.n_seq / 32);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += align_up(bytes, 256);
+        return here;
+    };
+    w.aux = take((size_t)a.n_q * a.h_q * 8);
+    w.part_q = take(w.q_parts > 1 ? (size_t)w.q_parts * a.n_q * a.h_q * d * 4 : 0);
+    w.part_k = take(w.k_parts > 1 ? (size_t)w.k_parts * a.n_k * a.h_kv * d * 4 : 0);
+    w.part_v = take(w.k_parts > 1 ? (size_t)w.k_parts * a.n_k * a.h_kv * d * 4 : 0);
+    w.part_bias = take(a.n_buckets > 0 ? (size_t)w.q_slots * a.h_q * a.n_buckets * 4 : 0);
+    w.total = at;
+    return w;
+}
+
+template <int D>
+lsrm_status launch_backward_d(AttnArgs a, void *ws, hipStream_t st) {
+    const bool bias = a.n_buckets > 0;
+    if (a.n_seq > 0) {
+        const WsLayout w = layout(a, D);
+        char *base = static_cast<char *>(ws);
+        a.aux = reinterpret_cast<float2 *>(base + w.aux);
+        a.part_q = reinterpret_cast<float *>(base + w.part_q);
+        a.part_k = reinterpret_cast<float *>(base + w.part_k);
+        a.part_v = reinterpret_cast<float *>(base + w.part_v);
+        a.part_bias = a.dbias != nullptr ? reinterpret_cast<float *>(base + w.part_bias) : nullptr;
+        const int n_tab = bias ? a.group * a.tab * 4 : 0;
+        a.n_slots = w.q_slots;
+        a.parts = w.q_parts;
+        lsrm_status rc = launch_attn(bias ? &attn_dq_kernel<D, true> : &attn_dq_kernel<D, false>, (int64_t)w.q_slots * a.h_kv * w.q_parts,
+                                     kDqLds<D> + (bias ? 5 * n_tab + 1024 : 0), a, st);
+        if (rc != LSRM_OK) return rc;
+        if (w.q_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, true>, (int64_t)(a.n_q / 128 + a.n_seq) * a.h_q, 0, a, st)) != LSRM_OK) return rc;
+        a.parts = w.k_parts;
+        rc = launch_attn(bias ? &attn_dkv_kernel<D, true> : &attn_dkv_kernel<D, false>, (int64_t)w.k_slots * a.h_kv * w.k_parts,
+                         kDkvLds<D> + n_tab, a, st);
+        if (rc != LSRM_OK) return rc;
+        if (w.k_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, false>, (int64_t)w.k_slots * a.h_kv, 0, a, st)) != LSRM_OK) return rc;
+    } else {
+        a.n_slots = 0;
+    }
+    if (bias && a.dbias != nullptr) return launch_attn(&attn_sum_bias, a.h_q, 0, a, st);
+    return LSRM_OK;
+}
+
+}  // namespace
+
+size_t attn_backward_ws_bytes(const AttnArgs &a, int d) { return a.n_seq > 0 ? layout(a, d).total : 0; }
+
+lsrm_status launch_attn_backward(AttnArgs a, int d, void *ws, hipStream_t st) {
+    switch (d) {
+        case 32: return launch_backward_d<32>(a, ws, st);
+        case 64: return launch_backward_d<64>(a, ws, st);
+        default: return launch_backward_d<128>(a, ws, st);
+    }
+}
+
+}  // namespace lsrm

@@ -1,0 +1,447 @@
+// Dense attention over packed sequences, forward, on gfx950.
+//
+// Per 32 keys and wavefront (32 query rows):  S^T = K Q^T (A = 32 key rows, B = Q^T), probabilities in registers (each lane owns one query
+// row, so maxima and sums are in-lane), O^T += V^T P^T (A = the transposed tile, read out of the row-major one by the transposing LDS
+// loads).  The running maximum is kept optimistically: the exponentials of a tile are taken against the present one and only their
+// sum is examined; a tile whose sum exceeds 2^10 is redone after raising the maximum.
+#include "attn_internal.h"
+
+#include <algorithm>
+
+namespace lsrm {
+
+namespace {
+
+constexpr float kMinusHuge = -3.2e38f;  // initial running maximum, in the exponent's unit: finite, so no inf - inf, and below any score
+constexpr float kSumLimit = 1024.0f;
+constexpr int kFewRows = 32;
+
+// The rows of one wavefront: 32 from row v0 of the sequence on.
+template <int D, bool BIAS>
+struct Rows {
+    bf16x8 q[AttnGeo<D>::NS];
+    f32x16 o[AttnGeo<D>::ND];
+    float m, l;
+    int lim;                // keys that this lane's row sees
+    int lim_min, lim_max;   // the fewest and most that a row of the wavefront sees
+    int pos, pos_min, pos_max;
+    const float *tab;       // expanded bias of this lane's head
+};
+template <int D, bool BIAS>
+__device__ __forceinline__ void load_rows(const AttnArgs &a, const Sequence &s, int head_kv, int v0, int lane, const float *tab, Rows<D, BIAS> &r) {
+    const int n_rows = s.n_q * a.group;
+    r.m = BIAS ? kMinusHuge : kMinusHuge / fmaxf(a.sl2, 1.0f);
+    r.l = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < AttnGeo<D>::ND; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) r.o[dt][i] = 0.f;
+    r.lim = r.lim_min = r.lim_max = r.pos = r.pos_min = r.pos_max = 0;
+    r.tab = tab;
+    if (v0 >= n_rows) {
+#pragma unroll
+        for (int ks = 0; ks < AttnGeo<D>::NS; ++ks) r.q[ks] = bf16x8{};
+        return;
+    }
+    // rows behind the last one do its work again; what they get is not written
+    const int last = min(v0 + 31, n_rows - 1), v = min(v0 + (lane & 31), last);
+    const int tok = (unsigned)v / (unsigned)a.group, g = v - tok * a.group;
+    r.pos = tok + s.shift;
+    r.pos_min = v0 / a.group + s.shift;
+    r.pos_max = last / a.group + s.shift;
+    auto seen = [&](int pos) { return a.causal ? min(max(pos + 1, 0), s.n_k) : s.n_k; };
+    r.lim = seen(r.pos);
+    r.lim_min = seen(r.pos_min);
+    r.lim_max = seen(r.pos_max);
+    if (BIAS) r.tab = tab + g * a.tab;
+    const uint16_t *q = a.q + (s.q0 + tok) * a.qs[0] + (int64_t)(head_kv * a.group + g) * a.qs[1] + 8 * (lane >> 5);
+#pragma unroll
+    for (int ks = 0; ks < AttnGeo<D>::NS; ++ks) r.q[ks] = *reinterpret_cast<const bf16x8 *>(q + 16 * ks);
+}
+
+// Scores, with a bias, are kept in the exponent's unit (times log2e); without one the factor goes into the exponential's argument.
+template <int D, bool BIAS>
+__device__ __forceinline__ void add_bias(const AttnArgs &a, const Rows<D, BIAS> &r, f32x16 &s, int j0, int hh) {
+    if (j0 + 31 - r.pos_min < a.b0 || j0 - r.pos_max >= a.b0 + a.tab - 2) {  // one bucket for the whole tile
+        const float c = r.tab[j0 - r.pos_max >= a.b0 + a.tab - 2 ? a.tab - 1 : 0];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = s[i] * a.sl2 + c;
+    } else {
+        const int x0 = j0 - r.pos - a.b0 + 1;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = s[i] * a.sl2 + r.tab[min(max(x0 + acc_row(i, hh), 0), a.tab - 1)];
+    }
+}
+
+// One tile of 32 keys from key j0 of the sequence on.
+template <int D, bool BIAS>
+__device__ __forceinline__ void attend(const AttnArgs &a, Rows<D, BIAS> &r, const char *kt, const char *vt, const TileLane<D> &t, int j0, int hh) {
+    f32x16 s;
+    mfma_rows<D>(s, kt, t, r.q);
+    const float sl = BIAS ? 1.0f : a.sl2;
+    if (BIAS) add_bias<D, BIAS>(a, r, s, j0, hh);
+    if (j0 + 32 > r.lim_min) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (j0 + acc_row(i, hh) >= r.lim) s[i] = -__builtin_inff();
+    }
+    f32x16 p;
+    float sum = 0.f, mc = r.m * sl;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(s[i] * sl - mc);
+        sum += p[i];
+    }
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kSumLimit)) != 0, 0)) {
+        mfma_settle();  // the accumulators of the tile before may be in flight
+        float mx = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+        const float m_new = fmaxf(r.m, half_max(mx));
+        const float alpha = __builtin_amdgcn_exp2f((r.m - m_new) * sl);
+        r.m = m_new;
+        r.l *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < AttnGeo<D>::ND; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) r.o[dt][i] *= alpha;
+        mc = m_new * sl;
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            p[i] = __builtin_amdgcn_exp2f(s[i] * sl - mc);
+            sum += p[i];
+        }
+    }
+    r.l += sum;
+    BFrag b[2];
+    to_b_operand(p, b);
+    mfma_transposed<D>(r.o, vt, t, b);
+}
+
+// ---- many rows: four wavefronts of 32 rows share the tiles ------------------------------------------------------------
+constexpr int kStage = 64;  // keys per stage
+template <int D>
+constexpr int kForwardLds = 2 * kStage * 2 * AttnGeo<D>::ROW;
+
+template <int D, bool BIAS>
+__global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
+    using G = AttnGeo<D>;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
+    const int head_kv = blockIdx.x % a.h_kv;
+    const int slot = a.causal ? a.n_slots - 1 - (int)(blockIdx.x / a.h_kv) : (int)(blockIdx.x / a.h_kv);
+    const int seq = find_sequence(a.q_off, a.n_q, a.n_seq, a.group, 128, slot);
+    const Sequence s = load_sequence(a, seq);
+    const int v0 = (slot - tile_slot(a.q_off, a.n_q, a.group, 128, seq)) * 128, slot_rows = s.q_slot * a.group;
+    if (v0 < 0 || v0 >= slot_rows) return;
+    const int n_rows = s.n_q * a.group;
+    int keys = 0;  // that the last live row sees, hence any
+    if (v0 < n_rows) {
+        const int last = min(v0 + 127, n_rows - 1) / a.group;
+        keys = a.causal ? min(max(last + s.shift + 1, 0), s.n_k) : s.n_k;
+    }
+    const int n_st = (keys + kStage - 1) / kStage;
+    const char *kb = reinterpret_cast<const char *>(a.k + s.k0 * a.ks[0] + head_kv * a.ks[1]);
+    const char *vb = reinterpret_cast<const char *>(a.v + s.k0 * a.vs[0] + head_kv * a.vs[1]);
+    const uint32_t k_row = (uint32_t)a.ks[0] * 2, v_row = (uint32_t)a.vs[0] * 2;
+    const CopyLane<D> c(lane);
+    auto copy_stage = [&](int st) {
+        char *at = lds + (st & 1) * (2 * kStage * G::ROW);
+        const int j0 = st * kStage;
+        copy_rows<D, kStage, 4>(kb + (uint64_t)j0 * k_row, k_row, keys - j0, at, wave, c);
+        copy_rows<D, kStage, 4>(vb + (uint64_t)j0 * v_row, v_row, keys - j0, at + kStage * G::ROW, wave, c);
+    };
+    if (n_st > 0) copy_stage(0);
+    float *tab = reinterpret_cast<float *>(lds + kForwardLds<D>);
+    if (BIAS) expand_bias(a, head_kv, tab, 256);
+    Rows<D, BIAS> r;
+    load_rows<D, BIAS>(a, s, head_kv, v0 + wave * 32, lane, tab, r);
+    const TileLane<D> t(lane);
+    for (int st = 0; st < n_st; ++st) {
+        wait_copies<0>();
+        wg_barrier();
+        if (st + 1 < n_st) copy_stage(st + 1);
+        const char *at = lds + (st & 1) * (2 * kStage * G::ROW);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (st * kStage + 32 * h < r.lim_max)
+                attend<D, BIAS>(a, r, at + h * G::TILE, at + (kStage + 32 * h) * G::ROW, t, st * kStage + 32 * h, hh);
+    }
+    wait_copies<0>();
+    wg_barrier();
+    mfma_settle();
+    const float l = half_sum(r.l), inv = l > 0.f || l != l ? 1.0f / l : 0.f;
+    const int row = v0 + wave * 32 + (lane & 31);
+    const bool live = row < n_rows;
+    store_query_rows<D>(a, s, head_kv, v0 + wave * 32, slot_rows, r.o, inv, live, lds + wave * 32 * G::OUT_ROW, a.out, a.os, lane);
+    if (a.lse != nullptr && hh == 0 && row < slot_rows) {
+        const int tok = (unsigned)row / (unsigned)a.group, g = row - tok * a.group;
+        a.lse[(int64_t)(s.q0 + tok) * a.h_q + head_kv * a.group + g] =
+            live && inv != 0.f ? (r.m * (BIAS ? 1.0f : a.sl2) + __builtin_amdgcn_logf(l)) * kLn2 : -__builtin_inff();
+    }
+}
+
+// ---- few rows: the wavefronts of a workgroup take turns at the keys of one tile of rows -------------------------------
+// Where there are too few tiles of rows to fill the chip, the keys are cut into parts too: a unit is (tile of 32 rows, part), a part
+// the same number of keys in all sequences, so that sequences of different lengths cost what they hold.  Every workgroup works that
+// number out from the lengths (there is no one to ask: offsets and lengths are in device memory and the host must not wait).
+struct Plan {
+    int chunk;  // keys per part
+};
+__device__ __forceinline__ int row_tiles(const AttnArgs &a, const Sequence &s) { return (s.q_slot * a.group + kFewRows - 1) / kFewRows; }
+__device__ __forceinline__ int parts_of(const Sequence &s, int chunk) { return max(1, (s.n_k + chunk - 1) / chunk); }
+__device__ __forceinline__ int part_keys(const AttnArgs &a) {
+    const int lane = threadIdx.x & 63;
+    int64_t keys = 0;
+    int tiles = 0;
+    for (int i = lane; i < a.n_seq; i += 64) {
+        const Sequence s = load_sequence(a, i);
+        tiles += row_tiles(a, s);
+        keys += (int64_t)row_tiles(a, s) * s.n_k;
+    }
+    for (int x = 32; x > 0; x /= 2) {
+        keys += __shfl_xor(keys, x);
+        tiles += __shfl_xor(tiles, x);
+    }
+    // sum over tiles of ceil(keys / chunk) <= keys / chunk + tiles <= unit_cap
+    const int room = max(a.unit_cap - tiles, 1);
+    return __builtin_amdgcn_readfirstlane(max(256, (int)((keys + room - 1) / room + 127) / 128 * 128));
+}
+// units of the sequences before s
+__device__ __forceinline__ int units_before(const AttnArgs &a, int seq, int chunk) {
+    int n = 0;
+    for (int i = threadIdx.x & 63; i < seq; i += 64) {
+        const Sequence s = load_sequence(a, i);
+        n += row_tiles(a, s) * parts_of(s, chunk);
+    }
+    for (int x = 32; x > 0; x /= 2) n += __shfl_xor(n, x);
+    return __builtin_amdgcn_readfirstlane(n);
+}
+// sequence of a unit (n_seq if there is none) and the unit's number within it
+__device__ __forceinline__ int unit_sequence(const AttnArgs &a, int unit, int chunk, int *within) {
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int i0 = 0; i0 < a.n_seq; i0 += 64) {
+        int n = 0;
+        if (i0 + lane < a.n_seq) {
+            const Sequence s = load_sequence(a, i0 + lane);
+            n = row_tiles(a, s) * parts_of(s, chunk);
+        }
+        int upto = n;
+        for (int x = 1; x < 64; x *= 2) {
+            const int y = __shfl_up(upto, x);
+            if (lane >= x) upto += y;
+        }
+        const uint64_t found = __builtin_amdgcn_ballot_w64(unit < base + upto);
+        if (found != 0) {
+            const int at = __builtin_ctzll(found);
+            *within = __builtin_amdgcn_readfirstlane(unit - base - __shfl(upto - n, at));
+            return i0 + at;
+        }
+        base += __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+    }
+    return a.n_seq;
+}
+
+template <int D>
+constexpr int kFewRing = 2 * 2 * AttnGeo<D>::TILE;  // per wavefront: two slots of a K and a V tile
+template <int D>
+constexpr int kFewLds = 4 * kFewRing<D> + 1024;
+template <int D>
+constexpr int kPartFloats = kFewRows * (D + 2);
+
+// Writes what one thread holds of a row: D / 8 channels from channel c0 on.
+template <int D>
+__device__ __forceinline__ void store_channels(const AttnArgs &a, const Sequence &s, int head_kv, int v, int c0, const float (&x)[D / 8], float m2,
+                                               float l) {
+    const bool live = v < s.n_q * a.group;
+    const float inv = live && (l > 0.f || l != l) ? 1.0f / l : 0.f;
+    const int tok = (unsigned)v / (unsigned)a.group, head = head_kv * a.group + v - tok * a.group;
+    uint32_t w[D / 16];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) w[i] = inv != 0.f ? pack_bf16(x[2 * i] * inv, x[2 * i + 1] * inv) : 0;
+    uint16_t *dst = a.out + (s.q0 + tok) * a.os[0] + (int64_t)head * a.os[1] + c0;
+#pragma unroll
+    for (int i = 0; i < D / 16; i += 2) *reinterpret_cast<uint2 *>(dst + 2 * i) = make_uint2(w[i], w[i + 1]);
+    if (a.lse != nullptr && c0 == 0)
+        a.lse[(int64_t)(s.q0 + tok) * a.h_q + head] = inv != 0.f ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -__builtin_inff();
+}
+
+template <int D, bool BIAS, bool SPLIT>
+__global__ __launch_bounds__(256, 1) void attn_few_kernel(AttnArgs a) {
+    using G = AttnGeo<D>;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
+    const int head_kv = blockIdx.x % a.h_kv, unit = blockIdx.x / a.h_kv;
+    int seq, tile, part = 0, n_parts = 1, chunk = 0;
+    if (SPLIT) {
+        chunk = part_keys(a);
+        int within;
+        seq = unit_sequence(a, unit, chunk, &within);
+        if (seq >= a.n_seq) return;
+        tile = within;
+    } else {
+        seq = find_sequence(a.q_off, a.n_q, a.n_seq, a.group, kFewRows, unit);
+        tile = unit - tile_slot(a.q_off, a.n_q, a.group, kFewRows, seq);
+    }
+    const Sequence s = load_sequence(a, seq);
+    if (SPLIT) {
+        n_parts = parts_of(s, chunk);
+        part = tile % n_parts;
+        tile /= n_parts;
+    }
+    const int v0 = tile * kFewRows, slot_rows = s.q_slot * a.group;
+    if (v0 < 0 || v0 >= slot_rows) return;
+    Rows<D, BIAS> r;
+    float *tab = reinterpret_cast<float *>(lds + kFewLds<D>);
+    load_rows<D, BIAS>(a, s, head_kv, v0, lane, tab, r);
+    const int j_begin = SPLIT ? part * chunk : 0, j_end = min(SPLIT ? j_begin + chunk : s.n_k, r.lim_max);
+    const char *kb = reinterpret_cast<const char *>(a.k + s.k0 * a.ks[0] + head_kv * a.ks[1]);
+    const char *vb = reinterpret_cast<const char *>(a.v + s.k0 * a.vs[0] + head_kv * a.vs[1]);
+    const uint32_t k_row = (uint32_t)a.ks[0] * 2, v_row = (uint32_t)a.vs[0] * 2;
+    const CopyLane<D> c(lane);
+    const TileLane<D> t(lane);
+    char *ring = lds + wave * kFewRing<D>;
+    auto copy_tile = [&](int j0, int slot) {
+        char *at = ring + slot * 2 * G::TILE;
+        copy_rows<D, 32, 1>(kb + (uint64_t)j0 * k_row, k_row, j_end - j0, at, 0, c);
+        copy_rows<D, 32, 1>(vb + (uint64_t)j0 * v_row, v_row, j_end - j0, at + G::TILE, 0, c);
+    };
+    int j0 = j_begin + wave * 32;
+    if (j0 < j_end) copy_tile(j0, 0);
+    if (BIAS) {
+        expand_bias(a, head_kv, tab, 256);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wg_barrier();
+    }
+    for (int slot = 0; j0 < j_end; j0 += 128, slot ^= 1) {
+        if (j0 + 128 < j_end) {
+            copy_tile(j0 + 128, slot ^ 1);
+            wait_copies<2 * G::COPIES>();
+        } else {
+            wait_copies<0>();
+        }
+        const char *at = ring + slot * 2 * G::TILE;
+        attend<D, BIAS>(a, r, at, at + G::TILE, t, j0, hh);
+    }
+    // the wavefronts' sums meet in LDS
+    mfma_settle();
+    constexpr int PITCH = D + 4;
+    float *mine = reinterpret_cast<float *>(ring), *ml = reinterpret_cast<float *>(lds + 4 * kFewRing<D>);
+    const float l = half_sum(r.l);
+#pragma unroll
+    for (int dt = 0; dt < G::ND; ++dt)
+#pragma unroll
+        for (int gq = 0; gq < 4; ++gq) {
+            f32x4 w = {r.o[dt][4 * gq], r.o[dt][4 * gq + 1], r.o[dt][4 * gq + 2], r.o[dt][4 * gq + 3]};
+            *reinterpret_cast<f32x4 *>(mine + (lane & 31) * PITCH + 32 * dt + 8 * gq + 4 * hh) = w;
+        }
+    if (hh == 0) {
+        ml[wave * 64 + lane] = r.m * (BIAS ? 1.0f : a.sl2);
+        ml[wave * 64 + 32 + lane] = l;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    wg_barrier();
+    const int row = threadIdx.x / 8, c0 = (threadIdx.x % 8) * (D / 8);
+    float m2 = ml[row], sum = 0.f, x[D / 8] = {};
+#pragma unroll
+    for (int w = 1; w < 4; ++w) m2 = fmaxf(m2, ml[w * 64 + row]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(ml[w * 64 + row] - m2);
+        sum += f * ml[w * 64 + 32 + row];
+        const float *from = reinterpret_cast<const float *>(lds + w * kFewRing<D>) + row * PITCH + c0;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) x[i] += f * from[i];
+    }
+    if (SPLIT && n_parts > 1) {
+        float *to = a.part + ((int64_t)unit * a.h_kv + head_kv) * kPartFloats<D>;
+#pragma unroll
+        for (int i = 0; i < D / 8; i += 4) *reinterpret_cast<f32x4 *>(to + row * D + c0 + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+        if (c0 == 0) {
+            to[kFewRows * D + row] = m2;
+            to[kFewRows * D + kFewRows + row] = sum;
+        }
+    } else if (v0 + row < slot_rows) {
+        store_channels<D>(a, s, head_kv, v0 + row, c0, x, m2, sum);
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
+    const int head_kv = blockIdx.x % a.h_kv, slot = blockIdx.x / a.h_kv;
+    const int seq = find_sequence(a.q_off, a.n_q, a.n_seq, a.group, kFewRows, slot);
+    const int tile = slot - tile_slot(a.q_off, a.n_q, a.group, kFewRows, seq);
+    const Sequence s = load_sequence(a, seq);
+    const int v = tile * kFewRows + threadIdx.x / 8, slot_rows = s.q_slot * a.group;
+    if (tile < 0 || tile * kFewRows >= slot_rows) return;
+    const int chunk = part_keys(a), n_parts = parts_of(s, chunk);
+    if (n_parts == 1) return;
+    const int unit = units_before(a, seq, chunk) + tile * n_parts;
+    if (unit < 0 || n_parts > a.unit_cap - unit) return;  // (of offsets that do not ascend)
+    const int row = threadIdx.x / 8, c0 = (threadIdx.x % 8) * (D / 8);
+    const float *from = a.part + ((int64_t)unit * a.h_kv + head_kv) * kPartFloats<D>;
+    const int64_t step = (int64_t)a.h_kv * kPartFloats<D>;
+    float m2 = kMinusHuge, sum = 0.f, x[D / 8] = {};
+    for (int p = 0; p < n_parts; ++p) {
+        const float *at = from + p * step;
+        const float m = at[kFewRows * D + row], l = at[kFewRows * D + kFewRows + row];
+        const float m_new = fmaxf(m2, m), f0 = __builtin_amdgcn_exp2f(m2 - m_new), f1 = __builtin_amdgcn_exp2f(m - m_new);
+        m2 = m_new;
+        sum = sum * f0 + l * f1;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) x[i] = x[i] * f0 + at[row * D + c0 + i] * f1;
+    }
+    if (v < slot_rows) store_channels<D>(a, s, head_kv, v, c0, x, m2, sum);
+}
+
+enum Way { MANY, FEW, FEW_SPLIT };
+// How a forward call is worked on.  slots32: tiles of 32 rows at most.
+Way forward_way(const AttnArgs &a, int64_t *slots32) {
+    const int64_t rows = (int64_t)a.n_q * a.group;
+    *slots32 = rows / kFewRows + a.n_seq;
+    if (rows >= (int64_t)64 * a.n_seq && (rows / 128 + 1) * a.h_kv >= 256) return MANY;
+    if (*slots32 * a.h_kv >= 1024 || a.n_k <= 512) return rows >= (int64_t)64 * a.n_seq && *slots32 * a.h_kv >= 1024 ? MANY : FEW;
+    return FEW_SPLIT;
+}
+int unit_cap(const AttnArgs &a, int64_t slots32) { return (int)std::max<int64_t>(2 * slots32, 1024 / a.h_kv); }
+
+template <int D>
+lsrm_status launch_forward_d(AttnArgs a, void *ws, hipStream_t st) {
+    int64_t slots32;
+    const Way way = forward_way(a, &slots32);
+    const int tab = a.n_buckets > 0 ? a.group * a.tab * 4 : 0;
+    const bool bias = a.n_buckets > 0;
+    if (way == MANY) {
+        a.n_slots = (int)((int64_t)a.n_q * a.group / 128 + a.n_seq);
+        return launch_attn(bias ? &attn_forward_kernel<D, true> : &attn_forward_kernel<D, false>, (int64_t)a.n_slots * a.h_kv,
+                           kForwardLds<D> + tab, a, st);
+    }
+    if (way == FEW)
+        return launch_attn(bias ? &attn_few_kernel<D, true, false> : &attn_few_kernel<D, false, false>, slots32 * a.h_kv, kFewLds<D> + tab, a, st);
+    a.unit_cap = unit_cap(a, slots32);
+    a.part = static_cast<float *>(ws);
+    lsrm_status rc = launch_attn(bias ? &attn_few_kernel<D, true, true> : &attn_few_kernel<D, false, true>, (int64_t)a.unit_cap * a.h_kv,
+                                 kFewLds<D> + tab, a, st);
+    if (rc != LSRM_OK) return rc;
+    return launch_attn(&attn_join_kernel<D>, slots32 * a.h_kv, 0, a, st);
+}
+
+}  // namespace
+
+size_t attn_forward_ws_bytes(const AttnArgs &a, int d) {
+    int64_t slots32;
+    if (a.n_seq == 0 || a.n_q == 0 || forward_way(a, &slots32) != FEW_SPLIT) return 0;
+    return (size_t)unit_cap(a, slots32) * a.h_kv * kFewRows * (d + 2) * 4;
+}
+
+lsrm_status launch_attn_forward(AttnArgs a, int d, void *ws, hipStream_t st) {
+    switch (d) {
+        case 32: return launch_forward_d<32>(a, ws, st);
+        case 64: return launch_forward_d<64>(a, ws, st);
+        default: return launch_forward_d<128>(a, ws, st);
+    }
+}
+
+}  // namespace lsrm

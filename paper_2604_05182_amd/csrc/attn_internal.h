@@ -1,0 +1,318 @@
+// What the forward and the backward of dense attention over packed sequences share: the problem's description, where a workgroup's
+// rows are, tiles in LDS and the MFMA operands read from them, the bias.  (gfx950)
+#pragma once
+#include "lsrm_internal.h"
+
+#include <utility>
+
+namespace lsrm {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kMaxBuckets = 64;
+constexpr int kMaxBiasEntries = 4096;  // of the expanded bias of a group of heads (in LDS: 16 KB, and four times that for its gradient)
+
+struct AttnArgs {
+    const uint16_t *q, *k, *v, *bias, *dout, *o;
+    uint16_t *out, *dq, *dk, *dv, *dbias;
+    const float *lse_in;
+    float *lse;
+    const int32_t *q_off, *k_off, *q_len, *k_len;
+    int64_t qs[2], ks[2], vs[2], os[2];  // {row, head} strides in elements
+    int n_q, n_k, n_seq, h_q, h_kv, group, causal;
+    int n_slots;           // row tiles of all sequences at most (see find_sequence)
+    int unit_cap;          // forward of few rows: units of all sequences at most
+    int parts;             // backward: parts that a walk is cut into
+    float *part;           // forward of few rows: sums of the parts
+    float2 *aux;           // backward: [h_q][n_q] {lse log2e (+inf for a query without keys), -D}
+    float *part_q, *part_k, *part_v, *part_bias;
+    int n_buckets, b0, tab;  // tab: entries of a head's expanded bias (0: no bias), for distances b0 - 1 .. b0 + tab - 2
+    int32_t bounds[kMaxBuckets - 1];
+    float scale, sl2;
+};
+
+// validates params; fills everything but the tensors
+lsrm_status make_attn_args(const lsrm_attn_params *p, AttnArgs *a);
+size_t attn_forward_ws_bytes(const AttnArgs &a, int d);
+size_t attn_backward_ws_bytes(const AttnArgs &a, int d);
+lsrm_status launch_attn_forward(AttnArgs a, int d, void *ws, hipStream_t st);
+lsrm_status launch_attn_backward(AttnArgs a, int d, void *ws, hipStream_t st);
+
+// ---- where a workgroup's rows are ------------------------------------------------------------------------------------
+// The query rows of a key/value head are numbered (query, head of its group), heads fastest: a tile of rows then reads a key or
+// value once for all heads that share it, single queries fill a tile with their heads, and a causal tile's rows see almost
+// the same keys.
+struct Sequence {
+    int q0, n_q, q_slot;  // first row, queries, rows of the slot
+    int k0, n_k, k_slot;
+    int shift;  // position of query 0
+};
+// (whatever the offsets and lengths hold, the rows lie in the tensors)
+__device__ __forceinline__ Sequence load_sequence(const AttnArgs &a, int s) {
+    Sequence r;
+    r.q0 = min(max(a.q_off[s], 0), a.n_q);
+    r.q_slot = min(max(a.q_off[s + 1], r.q0), a.n_q) - r.q0;
+    r.k0 = min(max(a.k_off[s], 0), a.n_k);
+    r.k_slot = min(max(a.k_off[s + 1], r.k0), a.n_k) - r.k0;
+    r.n_q = a.q_len != nullptr ? min(max(a.q_len[s], 0), r.q_slot) : r.q_slot;
+    r.n_k = a.k_len != nullptr ? min(max(a.k_len[s], 0), r.k_slot) : r.k_slot;
+    r.shift = r.n_k - r.n_q;
+    return r;
+}
+
+// Tiles of `bm` rows have slots of their own without anyone counting them: sequence s starts at slot floor(first row / bm) + s, and has
+// at most as many tiles as there are slots up to the next one's start.  Returns the last sequence that starts at or before slot x:
+// a wavefront probes 64 places at a time (one round up to 64 sequences, two up to 4096).
+__device__ __forceinline__ int tile_slot(const int32_t *off, int n_rows, int mult, int bm, int s) {
+    return min(max(off[s], 0), n_rows) * mult / bm + s;
+}
+__device__ __forceinline__ int find_sequence(const int32_t *off, int n_rows, int n_seq, int mult, int bm, int x) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = n_seq;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, s = lo + (lane + 1) * step;
+        const uint64_t below = __builtin_amdgcn_ballot_w64(s < hi && tile_slot(off, n_rows, mult, bm, s) <= x);
+        const int c = __builtin_ctzll(~below);  // (the last lane's place is never below hi)
+        lo += c * step;
+        hi = min(hi, lo + step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// ---- tiles in LDS ----------------------------------------------------------------------------------------------------
+// A tile is 32 rows of one head, row-major, as they are in memory; the 16-byte chunks of a row change places by a key of its row
+// number, so that reads of one chunk of many rows (MFMA operands along the channels) and of few chunks of four rows
+// (transposing reads) both spread over all banks.
+template <int D>
+struct AttnGeo {
+    static constexpr int NS = D / 16, ND = D / 32;  // 16-channel slabs, 32-channel tiles
+    static constexpr int ROW = 2 * D;               // bytes
+    static constexpr int TILE = 32 * ROW;
+    static constexpr int RPC = 1024 / ROW;          // rows per copy instruction
+    static constexpr int COPIES = TILE / 1024;      // copy instructions per tile
+    static constexpr int NX = NS < 4 ? NS : 4;      // addresses for reads along the channels
+    static constexpr int OUT_ROW = 2 * D + 16;      // padded row of the output staging (bytes)
+};
+template <int D>
+__device__ __forceinline__ int row_key(int r) {
+    const int b = ((r >> 2) ^ (r >> 3)) & 1;
+    return D == 32 ? (((r >> 1) & 1) << 1) | b : ((r & 3) << 1) | b;
+}
+// row permutation of the operand whose product becomes the next contraction's operand: bits 2 and 3 swapped
+__device__ __forceinline__ int perm32(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
+
+// Where this lane's 16 bytes of copy instruction i of a tile come from: row of the tile, byte in the row
+template <int D>
+struct CopyLane {
+    int row, chunk;  // of instruction 0; the others add i * RPC rows and xor the chunk's lowest bit (copy_flip)
+    __device__ explicit CopyLane(int lane) {
+        row = lane * 16 / AttnGeo<D>::ROW;
+        chunk = (lane * 16 % AttnGeo<D>::ROW) / 16 ^ row_key<D>(row);
+    }
+};
+template <int D>
+__device__ __forceinline__ constexpr int copy_flip(int i) {
+    return D == 128 ? (i ^ (i >> 1)) & 1 : D == 64 ? i & 1 : 0;
+}
+
+// Copies the instructions first, first + step, ... of n rows (a multiple of 32, tiles behind each other) from src, rows stride_b bytes apart, to
+// dst.  Rows from `avail` on (>= 1) are copies of row avail - 1: nothing behind a sequence's keys is ever read.
+template <int D, int N, int STEP>
+__device__ __forceinline__ void copy_rows(const char *src, uint32_t stride_b, int avail, const char *dst, int first, const CopyLane<D> &c) {
+    using G = AttnGeo<D>;
+    constexpr int N_COPY = N / G::RPC;
+    if (avail >= N) {
+#pragma unroll
+        for (int n = 0; n < N_COPY / STEP; ++n) {
+            const int i = first + n * STEP;
+            copy_kb_to_lds(src + (uint64_t)(i * G::RPC) * stride_b, c.row * stride_b + ((c.chunk ^ copy_flip<D>(i)) << 4), dst + i * 1024);
+        }
+    } else {
+#pragma unroll
+        for (int n = 0; n < N_COPY / STEP; ++n) {
+            const int i = first + n * STEP;
+            copy_kb_to_lds(src, min(i * G::RPC + c.row, avail - 1) * stride_b + ((c.chunk ^ copy_flip<D>(i)) << 4), dst + i * 1024);
+        }
+    }
+}
+
+// Addresses of MFMA A operands in a tile (add the tile's own):
+//   rows   fragment ks: lane (hh = lane / 32, r): row perm32(r), channels 16 ks + 8 hh + 0..7     at at[ks % 4] + 128 (ks / 4)
+//   transp fragment (ks2, dt): lane (hh, r): channel 32 dt + r, rows 16 ks2 + 8 hh + 0..7: two transposing loads of four rows
+//          (ds_read_b64_tr_b16: in each group of 16 lanes, lane j gets as element e the 16-bit element j % 4 of what lane
+//          4 e + j / 4 addressed), at tr[half][dt % 2] + 128 (dt / 2) + 16 ks2 rows
+template <int D>
+struct TileLane {
+    uint32_t at[AttnGeo<D>::NX], tr[2][AttnGeo<D>::ND < 2 ? 1 : 2];
+    __device__ explicit TileLane(int lane) {
+        using G = AttnGeo<D>;
+        const int hh = lane >> 5, r = perm32(lane & 31);
+#pragma unroll
+        for (int x = 0; x < G::NX; ++x) at[x] = r * G::ROW + (((2 * x + hh) ^ row_key<D>(r)) << 4);
+        const int s = lane & 15, half16 = (lane >> 4) & 1;
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+            for (int p = 0; p < (G::ND < 2 ? 1 : 2); ++p) {
+                const int row = 8 * hh + 4 * h2 + (s >> 2);
+                tr[h2][p] = row * G::ROW + (((4 * p + 2 * half16 + ((s & 3) >> 1)) ^ row_key<D>(row)) << 4) + ((s & 1) << 3);
+            }
+    }
+};
+
+union BFrag {
+    bf16x8 v;
+    uint32_t u[4];
+    i32x2 h[2];
+};
+
+template <int D>
+__device__ __forceinline__ bf16x8 read_row_frag(const char *tile, const TileLane<D> &t, int ks) {
+    return *reinterpret_cast<const bf16x8 *>(tile + t.at[ks % AttnGeo<D>::NX] + (ks / 4) * 128);
+}
+
+// acc = (rows of the tile) x b over all channels
+template <int D>
+__device__ __forceinline__ void mfma_rows(f32x16 &acc, const char *tile, const TileLane<D> &t, const bf16x8 (&b)[AttnGeo<D>::NS]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < AttnGeo<D>::NS; ++ks)
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_row_frag<D>(tile, t, ks), b[ks], acc, 0, 0, 0);
+}
+
+// The transposing loads are inline assembly: the compiler cannot tell that the builtin leaves alone what copies in flight
+// are filling, and would wait for all of those first.  Their results are waited for by hand, counted (LDS operations of a
+// wavefront complete in order; others in flight only make the waits longer).
+template <int OFF>
+__device__ __forceinline__ void tr_issue(BFrag &f, uint32_t a0, uint32_t a1) {
+    asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%4\n\tds_read_b64_tr_b16 %1, %3 offset:%4"
+                 : "=&v"(f.h[0]), "=&v"(f.h[1])
+                 : "v"(a0), "v"(a1), "n"(OFF)
+                 : "memory");
+}
+template <int N>
+__device__ __forceinline__ bf16x8 tr_take(BFrag &f) {
+    asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(f.h[0]), "+v"(f.h[1]) : "n"(N) : "memory");
+    return f.v;
+}
+// acc[dt] += (transposed tile: channels x 32 rows) x b[ks2] for every dt and ks2; all fragments requested at once, each MFMA waits for its own
+template <int D, int... I>
+__device__ __forceinline__ void mfma_transposed_impl(f32x16 (&acc)[AttnGeo<D>::ND], const uint32_t (&a0)[2], const uint32_t (&a1)[2],
+                                                     const BFrag (&b)[2], std::integer_sequence<int, I...>) {
+    constexpr int ND = AttnGeo<D>::ND;
+    BFrag f[2 * ND];
+    (tr_issue<(I % ND) / 2 * 128 + (I / ND) * 16 * AttnGeo<D>::ROW>(f[I], a0[(I % ND) % 2], a1[(I % ND) % 2]), ...);
+    ((acc[I % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_take<2 * (2 * ND - 1 - I)>(f[I]), b[I / ND].v, acc[I % ND], 0, 0, 0)), ...);
+}
+template <int D>
+__device__ __forceinline__ void mfma_transposed(f32x16 (&acc)[AttnGeo<D>::ND], const char *tile, const TileLane<D> &t, const BFrag (&b)[2]) {
+    const uint32_t at = (uint32_t)(uintptr_t)tile;  // (the low 32 bits of a generic pointer into LDS are the LDS address)
+    constexpr int P1 = AttnGeo<D>::ND < 2 ? 0 : 1;
+    const uint32_t a0[2] = {at + t.tr[0][0], at + t.tr[0][P1]}, a1[2] = {at + t.tr[1][0], at + t.tr[1][P1]};
+    mfma_transposed_impl<D>(acc, a0, a1, b, std::make_integer_sequence<int, 2 * AttnGeo<D>::ND>{});
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    bf16x2 p;
+    p[0] = (__bf16)a;
+    p[1] = (__bf16)b;
+    return *reinterpret_cast<uint32_t *>(&p);
+}
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// accumulator tile -> the two B operands (16-row slabs) of the next contraction
+__device__ __forceinline__ void to_b_operand(const f32x16 &x, BFrag (&b)[2]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) b[k / 4].u[k % 4] = pack_bf16(x[2 * k], x[2 * k + 1]);
+}
+// row of a tile that accumulator element i of a product with permuted rows belongs to
+__device__ __forceinline__ int acc_row(int i, int hh) { return 16 * (i / 8) + 8 * hh + i % 8; }
+
+// max / sum across the two lane halves (lanes i and i + 32 hold the same column)
+__device__ __forceinline__ float half_max(float x) {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// s_waitcnt vmcnt <= n and lgkmcnt == 0; a bare barrier: who copied waits for the copies before it
+constexpr int vm_lgkm_imm(int n) { return (n & 0xF) | ((n >> 4) << 14) | 0x0070; }
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(vm_lgkm_imm(N));
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wg_barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+// Results of an MFMA become readable by VALU instructions a fixed number of cycles after issue; the compiler pads, but not reliably where a
+// branch lies between.  24 wait states cover the 8 passes.
+__device__ __forceinline__ void mfma_settle() { asm volatile("s_nop 15\n\ts_nop 7" ::: "memory"); }
+
+// x (transposed: channels x the 32 rows from v0 on, times mul; zeros in rows that are not live) -> bf16 rows of a tensor of query rows, through
+// `stage` (32 OUT_ROW bytes of the wavefront's own), so that they are written in 16-byte pieces
+template <int D>
+__device__ __forceinline__ void store_query_rows(const AttnArgs &a, const Sequence &s, int head_kv, int v0, int slot_rows,
+                                                 const f32x16 (&x)[AttnGeo<D>::ND], float mul, bool live, char *stage, uint16_t *dst,
+                                                 const int64_t (&stride)[2], int lane) {
+    using G = AttnGeo<D>;
+#pragma unroll
+    for (int dt = 0; dt < G::ND; ++dt)
+#pragma unroll
+        for (int gq = 0; gq < 4; ++gq) {
+            uint2 w;
+            w.x = live ? pack_bf16(x[dt][4 * gq] * mul, x[dt][4 * gq + 1] * mul) : 0;
+            w.y = live ? pack_bf16(x[dt][4 * gq + 2] * mul, x[dt][4 * gq + 3] * mul) : 0;
+            *reinterpret_cast<uint2 *>(stage + (lane & 31) * G::OUT_ROW + (32 * dt + 8 * gq + 4 * (lane >> 5)) * 2) = w;
+        }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    constexpr int CH = D / 8, RPP = 64 / CH;
+#pragma unroll
+    for (int it = 0; it < 32 / RPP; ++it) {
+        const int rr = it * RPP + lane / CH, v = v0 + rr;
+        if (v < slot_rows) {
+            const int tok = (unsigned)v / (unsigned)a.group, g = v - tok * a.group;
+            *reinterpret_cast<uint4 *>(dst + (s.q0 + tok) * stride[0] + (int64_t)(head_kv * a.group + g) * stride[1] + 8 * (lane % CH)) =
+                *reinterpret_cast<const uint4 *>(stage + rr * G::OUT_ROW + (lane % CH) * 16);
+        }
+    }
+}
+
+template <typename F>
+lsrm_status launch_attn(F kernel, int64_t grid, int lds, const AttnArgs &a, hipStream_t st) {
+    // (set on every call: cheap, and right whichever device is current and whichever thread calls)
+    if (lds > 64 * 1024)
+        LSRM_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), lds, st, a);
+    LSRM_HIP_CHECK(hipGetLastError());
+    return LSRM_OK;
+}
+
+// ---- the bias --------------------------------------------------------------------------------------------------------
+// The bias of one key/value head's query heads, expanded by distance, times log2e: entry x of a head is for the distance b0 - 1 + x,
+// the first for everything before, the last for everything behind.  -1e30 and below mask their bucket.
+__device__ __forceinline__ int bucket_of(const AttnArgs &a, int rel) {
+    int b = 0;
+    for (int i = 0; i < a.n_buckets - 1; ++i) b += a.bounds[i] <= rel;
+    return b;
+}
+__device__ __forceinline__ void expand_bias(const AttnArgs &a, int head_kv, float *tab, int threads) {
+    for (int x = threadIdx.x; x < a.tab; x += threads) {
+        const int b = bucket_of(a, a.b0 - 1 + x);
+        for (int g = 0; g < a.group; ++g) {
+            const float y = __uint_as_float((uint32_t)a.bias[(int64_t)(head_kv * a.group + g) * a.n_buckets + b] << 16);
+            tab[g * a.tab + x] = y <= -1.0e30f ? -__builtin_inff() : y * kLog2e;
+        }
+    }
+}
+
+}  // namespace lsrm
