@@ -472,19 +472,19 @@ lsrm_status launch_backward_d(AttnArgs a, void *ws, hipStream_t st) {
         const int n_tab = bias ? a.group * a.tab * 4 : 0;
         a.n_slots = w.q_slots;
         a.parts = w.q_parts;
-        lsrm_status rc = launch_attn(bias ? &attn_dq_kernel<D, true> : &attn_dq_kernel<D, false>, (int64_t)w.q_slots * a.h_kv * w.q_parts,
+        lsrm_status rc = launch_attn(bias ? &attn_dq_kernel<D, true> : &attn_dq_kernel<D, false>, (int64_t)w.q_slots * a.h_kv * w.q_parts, 256,
                                      kDqLds<D> + (bias ? 5 * n_tab + 1024 : 0), a, st);
         if (rc != LSRM_OK) return rc;
-        if (w.q_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, true>, (int64_t)(a.n_q / 128 + a.n_seq) * a.h_q, 0, a, st)) != LSRM_OK) return rc;
+        if (w.q_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, true>, (int64_t)(a.n_q / 128 + a.n_seq) * a.h_q, 256, 0, a, st)) != LSRM_OK) return rc;
         a.parts = w.k_parts;
-        rc = launch_attn(bias ? &attn_dkv_kernel<D, true> : &attn_dkv_kernel<D, false>, (int64_t)w.k_slots * a.h_kv * w.k_parts,
+        rc = launch_attn(bias ? &attn_dkv_kernel<D, true> : &attn_dkv_kernel<D, false>, (int64_t)w.k_slots * a.h_kv * w.k_parts, 256,
                          kDkvLds<D> + n_tab, a, st);
         if (rc != LSRM_OK) return rc;
-        if (w.k_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, false>, (int64_t)w.k_slots * a.h_kv, 0, a, st)) != LSRM_OK) return rc;
+        if (w.k_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, false>, (int64_t)w.k_slots * a.h_kv, 256, 0, a, st)) != LSRM_OK) return rc;
     } else {
         a.n_slots = 0;
     }
-    if (bias && a.dbias != nullptr) return launch_attn(&attn_sum_bias, a.h_q, 0, a, st);
+    if (bias && a.dbias != nullptr) return launch_attn(&attn_sum_bias, a.h_q, 256, 0, a, st);
     return LSRM_OK;
 }
 

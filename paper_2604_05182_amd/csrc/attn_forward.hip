@@ -244,33 +244,40 @@ __device__ __forceinline__ int unit_sequence(const AttnArgs &a, int unit, int ch
     return a.n_seq;
 }
 
+// Wavefronts of a workgroup.  Each has a ring of two slots (a K and a V tile) of its own; two workgroups share a CU at d = 128 too, so that
+// one streams while the other starts or ends.
 template <int D>
-constexpr int kFewRing = 2 * 2 * AttnGeo<D>::TILE;  // per wavefront: two slots of a K and a V tile
+constexpr int kFewWaves = D == 128 ? 2 : 4;
 template <int D>
-constexpr int kFewLds = 4 * kFewRing<D> + 1024;
+constexpr int kFewRing = 2 * 2 * AttnGeo<D>::TILE;  // per wavefront
+template <int D>
+constexpr int kFewLds = kFewWaves<D> * (kFewRing<D> + 256);
 template <int D>
 constexpr int kPartFloats = kFewRows * (D + 2);
 
-// Writes what one thread holds of a row: D / 8 channels from channel c0 on.
-template <int D>
-__device__ __forceinline__ void store_channels(const AttnArgs &a, const Sequence &s, int head_kv, int v, int c0, const float (&x)[D / 8], float m2,
+// Writes N channels of a row from channel c0 on.
+template <int N>
+__device__ __forceinline__ void store_channels(const AttnArgs &a, const Sequence &s, int head_kv, int v, int c0, const float (&x)[N], float m2,
                                                float l) {
     const bool live = v < s.n_q * a.group;
     const float inv = live && (l > 0.f || l != l) ? 1.0f / l : 0.f;
     const int tok = (unsigned)v / (unsigned)a.group, head = head_kv * a.group + v - tok * a.group;
-    uint32_t w[D / 16];
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) w[i] = inv != 0.f ? pack_bf16(x[2 * i] * inv, x[2 * i + 1] * inv) : 0;
     uint16_t *dst = a.out + (s.q0 + tok) * a.os[0] + (int64_t)head * a.os[1] + c0;
 #pragma unroll
-    for (int i = 0; i < D / 16; i += 2) *reinterpret_cast<uint2 *>(dst + 2 * i) = make_uint2(w[i], w[i + 1]);
+    for (int i = 0; i < N; i += 4) {
+        uint2 w;
+        w.x = inv != 0.f ? pack_bf16(x[i] * inv, x[i + 1] * inv) : 0;
+        w.y = inv != 0.f ? pack_bf16(x[i + 2] * inv, x[i + 3] * inv) : 0;
+        *reinterpret_cast<uint2 *>(dst + i) = w;
+    }
     if (a.lse != nullptr && c0 == 0)
         a.lse[(int64_t)(s.q0 + tok) * a.h_q + head] = inv != 0.f ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -__builtin_inff();
 }
 
 template <int D, bool BIAS, bool SPLIT>
-__global__ __launch_bounds__(256, 1) void attn_few_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves<D>, 1) void attn_few_kernel(AttnArgs a) {
     using G = AttnGeo<D>;
+    constexpr int NW = kFewWaves<D>, STEP = 32 * NW;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv, unit = blockIdx.x / a.h_kv;
@@ -311,13 +318,13 @@ __global__ __launch_bounds__(256, 1) void attn_few_kernel(AttnArgs a) {
     int j0 = j_begin + wave * 32;
     if (j0 < j_end) copy_tile(j0, 0);
     if (BIAS) {
-        expand_bias(a, head_kv, tab, 256);
+        expand_bias(a, head_kv, tab, 64 * NW);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         wg_barrier();
     }
-    for (int slot = 0; j0 < j_end; j0 += 128, slot ^= 1) {
-        if (j0 + 128 < j_end) {
-            copy_tile(j0 + 128, slot ^ 1);
+    for (int slot = 0; j0 < j_end; j0 += STEP, slot ^= 1) {
+        if (j0 + STEP < j_end) {
+            copy_tile(j0 + STEP, slot ^ 1);
             wait_copies<2 * G::COPIES>();
         } else {
             wait_copies<0>();
@@ -328,7 +335,7 @@ __global__ __launch_bounds__(256, 1) void attn_few_kernel(AttnArgs a) {
     // the wavefronts' sums meet in LDS
     mfma_settle();
     constexpr int PITCH = D + 4;
-    float *mine = reinterpret_cast<float *>(ring), *ml = reinterpret_cast<float *>(lds + 4 * kFewRing<D>);
+    float *mine = reinterpret_cast<float *>(ring), *ml = reinterpret_cast<float *>(lds + NW * kFewRing<D>);
     const float l = half_sum(r.l);
 #pragma unroll
     for (int dt = 0; dt < G::ND; ++dt)
@@ -343,57 +350,79 @@ __global__ __launch_bounds__(256, 1) void attn_few_kernel(AttnArgs a) {
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     wg_barrier();
-    const int row = threadIdx.x / 8, c0 = (threadIdx.x % 8) * (D / 8);
-    float m2 = ml[row], sum = 0.f, x[D / 8] = {};
+    constexpr int TPR = 2 * NW, CH = D / TPR;  // threads per row, channels per thread
+    const int row = threadIdx.x / TPR, c0 = (threadIdx.x % TPR) * CH;
+    if (v0 + row >= slot_rows) return;
+    float m2 = ml[row], sum = 0.f, x[CH] = {};
 #pragma unroll
-    for (int w = 1; w < 4; ++w) m2 = fmaxf(m2, ml[w * 64 + row]);
+    for (int w = 1; w < NW; ++w) m2 = fmaxf(m2, ml[w * 64 + row]);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
         const float f = __builtin_amdgcn_exp2f(ml[w * 64 + row] - m2);
         sum += f * ml[w * 64 + 32 + row];
         const float *from = reinterpret_cast<const float *>(lds + w * kFewRing<D>) + row * PITCH + c0;
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) x[i] += f * from[i];
+        for (int i = 0; i < CH; ++i) x[i] += f * from[i];
     }
     if (SPLIT && n_parts > 1) {
         float *to = a.part + ((int64_t)unit * a.h_kv + head_kv) * kPartFloats<D>;
 #pragma unroll
-        for (int i = 0; i < D / 8; i += 4) *reinterpret_cast<f32x4 *>(to + row * D + c0 + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+        for (int i = 0; i < CH; i += 4) *reinterpret_cast<f32x4 *>(to + row * D + c0 + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
         if (c0 == 0) {
             to[kFewRows * D + row] = m2;
             to[kFewRows * D + kFewRows + row] = sum;
         }
-    } else if (v0 + row < slot_rows) {
-        store_channels<D>(a, s, head_kv, v0 + row, c0, x, m2, sum);
+    } else {
+        store_channels<CH>(a, s, head_kv, v0 + row, c0, x, m2, sum);
     }
 }
 
+// Joins the parts of a tile's rows: a workgroup takes every eighth row, one after the other, four channels to a lane and the parts dealt to
+// 1024 / d groups of lanes.
+constexpr int kJoinWays = 8;
 template <int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
-    const int head_kv = blockIdx.x % a.h_kv, slot = blockIdx.x / a.h_kv;
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+    __shared__ f32x4 sums[GROUPS][LANES];
+    __shared__ float part_max[4], part_sum[4];
+    const int way = blockIdx.x % kJoinWays, head_kv = blockIdx.x / kJoinWays % a.h_kv, slot = blockIdx.x / kJoinWays / a.h_kv;
     const int seq = find_sequence(a.q_off, a.n_q, a.n_seq, a.group, kFewRows, slot);
     const int tile = slot - tile_slot(a.q_off, a.n_q, a.group, kFewRows, seq);
     const Sequence s = load_sequence(a, seq);
-    const int v = tile * kFewRows + threadIdx.x / 8, slot_rows = s.q_slot * a.group;
-    if (tile < 0 || tile * kFewRows >= slot_rows) return;
+    const int slot_rows = s.q_slot * a.group;
+    if (tile < 0 || tile * kFewRows + way >= slot_rows) return;
     const int chunk = part_keys(a), n_parts = parts_of(s, chunk);
     if (n_parts == 1) return;
     const int unit = units_before(a, seq, chunk) + tile * n_parts;
     if (unit < 0 || n_parts > a.unit_cap - unit) return;  // (of offsets that do not ascend)
-    const int row = threadIdx.x / 8, c0 = (threadIdx.x % 8) * (D / 8);
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, wave = threadIdx.x / 64;
     const float *from = a.part + ((int64_t)unit * a.h_kv + head_kv) * kPartFloats<D>;
     const int64_t step = (int64_t)a.h_kv * kPartFloats<D>;
-    float m2 = kMinusHuge, sum = 0.f, x[D / 8] = {};
-    for (int p = 0; p < n_parts; ++p) {
-        const float *at = from + p * step;
-        const float m = at[kFewRows * D + row], l = at[kFewRows * D + kFewRows + row];
-        const float m_new = fmaxf(m2, m), f0 = __builtin_amdgcn_exp2f(m2 - m_new), f1 = __builtin_amdgcn_exp2f(m - m_new);
-        m2 = m_new;
-        sum = sum * f0 + l * f1;
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) x[i] = x[i] * f0 + at[row * D + c0 + i] * f1;
+    for (int row = way; row < kFewRows && tile * kFewRows + row < slot_rows; row += kJoinWays) {
+        const float *ml = from + kFewRows * D + row;
+        float m2 = kMinusHuge;
+        for (int p = threadIdx.x; p < n_parts; p += 256) m2 = fmaxf(m2, ml[p * step]);
+        for (int x = 32; x > 0; x /= 2) m2 = fmaxf(m2, __shfl_xor(m2, x));
+        if (threadIdx.x % 64 == 0) part_max[wave] = m2;
+        __syncthreads();
+        m2 = fmaxf(fmaxf(part_max[0], part_max[1]), fmaxf(part_max[2], part_max[3]));
+        float sum = 0.f;
+        for (int p = threadIdx.x; p < n_parts; p += 256) sum += ml[p * step + kFewRows] * __builtin_amdgcn_exp2f(ml[p * step] - m2);
+        for (int x = 32; x > 0; x /= 2) sum += __shfl_xor(sum, x);
+        if (threadIdx.x % 64 == 0) part_sum[wave] = sum;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int p = group; p < n_parts; p += GROUPS)
+            acc += __builtin_amdgcn_exp2f(ml[p * step] - m2) * *reinterpret_cast<const f32x4 *>(from + p * step + row * D + 4 * lane);
+        sums[group][lane] = acc;
+        __syncthreads();
+        if (group == 0) {
+            for (int i = 1; i < GROUPS; ++i) acc += sums[i][lane];
+            const float x[4] = {acc[0], acc[1], acc[2], acc[3]};
+            store_channels<4>(a, s, head_kv, tile * kFewRows + row, 4 * lane, x, m2, part_sum[0] + part_sum[1] + part_sum[2] + part_sum[3]);
+        }
+        __syncthreads();
     }
-    if (v < slot_rows) store_channels<D>(a, s, head_kv, v, c0, x, m2, sum);
 }
 
 enum Way { MANY, FEW, FEW_SPLIT };
@@ -402,10 +431,11 @@ Way forward_way(const AttnArgs &a, int64_t *slots32) {
     const int64_t rows = (int64_t)a.n_q * a.group;
     *slots32 = rows / kFewRows + a.n_seq;
     if (rows >= (int64_t)64 * a.n_seq && (rows / 128 + 1) * a.h_kv >= 256) return MANY;
-    if (*slots32 * a.h_kv >= 1024 || a.n_k <= 512) return rows >= (int64_t)64 * a.n_seq && *slots32 * a.h_kv >= 1024 ? MANY : FEW;
-    return FEW_SPLIT;
+    if (*slots32 * a.h_kv >= 512) return rows >= (int64_t)64 * a.n_seq ? MANY : FEW;
+    return a.n_k / a.n_seq <= 1024 ? FEW : FEW_SPLIT;
 }
-int unit_cap(const AttnArgs &a, int64_t slots32) { return (int)std::max<int64_t>(2 * slots32, 1024 / a.h_kv); }
+// Units that the keys are cut into, per key/value head: two workgroups for every CU, or twice the tiles where there are many.
+int unit_cap(const AttnArgs &a, int64_t slots32) { return (int)std::max<int64_t>(2 * slots32, 512 / a.h_kv); }
 
 template <int D>
 lsrm_status launch_forward_d(AttnArgs a, void *ws, hipStream_t st) {
@@ -415,17 +445,18 @@ lsrm_status launch_forward_d(AttnArgs a, void *ws, hipStream_t st) {
     const bool bias = a.n_buckets > 0;
     if (way == MANY) {
         a.n_slots = (int)((int64_t)a.n_q * a.group / 128 + a.n_seq);
-        return launch_attn(bias ? &attn_forward_kernel<D, true> : &attn_forward_kernel<D, false>, (int64_t)a.n_slots * a.h_kv,
+        return launch_attn(bias ? &attn_forward_kernel<D, true> : &attn_forward_kernel<D, false>, (int64_t)a.n_slots * a.h_kv, 256,
                            kForwardLds<D> + tab, a, st);
     }
     if (way == FEW)
-        return launch_attn(bias ? &attn_few_kernel<D, true, false> : &attn_few_kernel<D, false, false>, slots32 * a.h_kv, kFewLds<D> + tab, a, st);
+        return launch_attn(bias ? &attn_few_kernel<D, true, false> : &attn_few_kernel<D, false, false>, slots32 * a.h_kv, 64 * kFewWaves<D>,
+                           kFewLds<D> + tab, a, st);
     a.unit_cap = unit_cap(a, slots32);
     a.part = static_cast<float *>(ws);
     lsrm_status rc = launch_attn(bias ? &attn_few_kernel<D, true, true> : &attn_few_kernel<D, false, true>, (int64_t)a.unit_cap * a.h_kv,
-                                 kFewLds<D> + tab, a, st);
+                                 64 * kFewWaves<D>, kFewLds<D> + tab, a, st);
     if (rc != LSRM_OK) return rc;
-    return launch_attn(&attn_join_kernel<D>, slots32 * a.h_kv, 0, a, st);
+    return launch_attn(&attn_join_kernel<D>, slots32 * a.h_kv * kJoinWays, 256, 0, a, st);
 }
 
 }  // namespace

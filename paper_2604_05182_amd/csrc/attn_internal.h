@@ -288,11 +288,11 @@ __device__ __forceinline__ void store_query_rows(const AttnArgs &a, const Sequen
 }
 
 template <typename F>
-lsrm_status launch_attn(F kernel, int64_t grid, int lds, const AttnArgs &a, hipStream_t st) {
+lsrm_status launch_attn(F kernel, int64_t grid, int threads, int lds, const AttnArgs &a, hipStream_t st) {
     // (set on every call: cheap, and right whichever device is current and whichever thread calls)
     if (lds > 64 * 1024)
         LSRM_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), lds, st, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), lds, st, a);
     LSRM_HIP_CHECK(hipGetLastError());
     return LSRM_OK;
 }
