@@ -344,8 +344,8 @@ typedef struct lsrm_attn_params {
     int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];
     int32_t n_buckets;            /* 0: no bias; else buckets of the bias, 1 .. 64                         */
     const int32_t *bucket_bounds; /* HOST, read during the call, [n_buckets - 1]: strictly ascending distances at which
-                                     the next bucket begins, within +-2^20;
-                                     (h_q / h_kv) * (last - first + 2) is at most 4096                     */
+                                     the next bucket begins, within +-2^20; last - first at most
+                                     1022, (h_q / h_kv) * (last - first + 130) at most 10240               */
 } lsrm_attn_params;
 
 /* Bytes of scratch for lsrm_attn_forward (LSRM_WS_FORWARD) or lsrm_attn_backward (LSRM_WS_BACKWARD); 0 on invalid

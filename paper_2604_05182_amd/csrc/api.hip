@@ -132,7 +132,9 @@ lsrm_status make_attn_args(const lsrm_attn_params *p, AttnArgs *a) {
             if (i > 0 && a->bounds[i] <= a->bounds[i - 1]) return LSRM_ERR_INVALID_ARG;
         }
         a->b0 = p->n_buckets > 1 ? a->bounds[0] : 0;
-        a->tab = p->n_buckets > 1 ? a->bounds[p->n_buckets - 2] - a->b0 + 2 : 2;
+        a->b_last = p->n_buckets > 1 ? a->bounds[p->n_buckets - 2] : 0;
+        if (a->b_last - a->b0 > kMaxBiasSpan) return LSRM_ERR_UNSUPPORTED;
+        a->tab = a->b_last - a->b0 + 2 + 2 * kBiasPad;
         if ((int64_t)a->group * a->tab > kMaxBiasEntries) return LSRM_ERR_UNSUPPORTED;
     }
     return LSRM_OK;

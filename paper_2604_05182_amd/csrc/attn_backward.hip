@@ -20,12 +20,11 @@ template <int D>
 constexpr int kDqLds = 2 * kStage * 2 * AttnGeo<D>::ROW;
 template <int D>
 constexpr int kDkvSlot = 2 * AttnGeo<D>::TILE + 256;  // 32 rows of q, of dout, and their entries of aux
+// Slots of the dK/dV pass' ring: below d = 128 a step takes less time than a copy under way, so two more are.
 template <int D>
-constexpr int kDkvLds = 4 * 32 * AttnGeo<D>::OUT_ROW > 2 * kDkvSlot<D> ? 4 * 32 * AttnGeo<D>::OUT_ROW : 2 * kDkvSlot<D>;
-
-__device__ __forceinline__ void lds_add(float *at, float x) {
-    asm volatile("ds_add_f32 %0, %1" ::"v"((uint32_t)(uintptr_t)at), "v"(x) : "memory");
-}
+constexpr int kDkvRing = D == 128 ? 2 : 4;
+template <int D>
+constexpr int kDkvLds = 4 * 32 * AttnGeo<D>::OUT_ROW > kDkvRing<D> * kDkvSlot<D> ? 4 * 32 * AttnGeo<D>::OUT_ROW : kDkvRing<D> * kDkvSlot<D>;
 
 template <int D, bool BIAS>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
@@ -39,12 +38,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     const Sequence s = load_sequence(a, seq);
     const int v_wg = (slot - tile_slot(a.q_off, a.n_q, a.group, 128, seq)) * 128, slot_rows = s.q_slot * a.group;
     const int n_rows = s.n_q * a.group;
-    if (v_wg < 0 || v_wg >= slot_rows) {
-        if (BIAS && a.part_bias != nullptr)
-            for (int i = threadIdx.x; i < a.group * a.n_buckets; i += 256)
-                a.part_bias[((int64_t)slot * a.h_q + head_kv * a.group) * a.n_buckets + i] = 0.f;
-        return;
-    }
+    if (v_wg < 0 || v_wg >= slot_rows) return;
     auto seen = [&](int pos) { return a.causal ? min(max(pos + 1, 0), s.n_k) : s.n_k; };
     const int keys = v_wg < n_rows ? seen(min(v_wg + 127, n_rows - 1) / a.group + s.shift) : 0;
     const int st_all = (keys + kStage - 1) / kStage, st_per = (st_all + a.parts - 1) / a.parts;
@@ -60,14 +54,8 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
         copy_rows<D, kStage, 4>(vb + (uint64_t)j0 * v_row, v_row, keys - j0, at + kStage * G::ROW, wave, c);
     };
     if (st_begin < st_end) copy_stage(st_begin);
-    // bias: expanded, then the sums of dS by distance of each wavefront, then what a workgroup ends with
     float *tab = reinterpret_cast<float *>(lds + kDqLds<D>);
-    const int n_tab = a.group * a.tab;
-    float *near = tab + (1 + wave) * n_tab, *far = tab + 5 * n_tab;
-    if (BIAS) {
-        expand_bias(a, head_kv, tab, 256);
-        for (int i = threadIdx.x; i < 4 * n_tab; i += 256) tab[n_tab + i] = 0.f;
-    }
+    if (BIAS) expand_bias(a, head_kv, tab, 256);
 
     const int v0 = v_wg + wave * 32, v = v0 + (lane & 31);
     const bool live = v < n_rows;
@@ -91,7 +79,6 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
         delta = half_sum(delta);
         const float lse = a.lse_in[(int64_t)(s.q0 + tok) * a.h_q + head];
         if (live && lse != -__builtin_inff()) off = lse * kLog2e;
-        if (live && hh == 0 && part == 0) a.aux[(int64_t)head * a.n_q + s.q0 + tok] = make_float2(off, -delta);
     } else {
 #pragma unroll
         for (int ks = 0; ks < G::NS; ++ks) q[ks] = dout[ks] = bf16x8{};
@@ -101,9 +88,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     for (int dt = 0; dt < G::ND; ++dt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) dq[dt][i] = 0.f;
-    // of this lane's row: sums of dS over all keys, and of dS and P over those before the first and behind the last bound
-    float sum_all = 0.f, sum_lo = 0.f, sum_hi = 0.f, p_lo = 0.f, p_hi = 0.f;
-    const int b_last = a.b0 + a.tab - 2;
+    float miss = 0.f;  // sum of dS over this lane's keys
     const float *tab_g = tab + g * a.tab;
     const TileLane<D> t(lane);
     for (int st = st_begin; st < st_end; ++st) {
@@ -119,16 +104,16 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
             f32x16 x, dp;
             mfma_rows<D>(x, kt, t, q);
             mfma_rows<D>(dp, vt, t, dout);
-            const bool behind = BIAS && j0 + 31 - pos_min < a.b0, ahead = BIAS && j0 - pos_max >= b_last;
-            const int x0 = j0 - pos - a.b0 + 1;
+            const bool behind = BIAS && j0 + 31 - pos_min < a.b0, ahead = BIAS && j0 - pos_max >= a.b_last;
             if (BIAS) {
                 if (behind || ahead) {
                     const float b = tab_g[ahead ? a.tab - 1 : 0];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[i] = x[i] * a.sl2 + b;
                 } else {
+                    const float *entry = tab_g + bias_entry(a, j0 - pos) + 8 * hh;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = x[i] * a.sl2 + tab_g[min(max(x0 + acc_row(i, hh), 0), a.tab - 1)];
+                    for (int i = 0; i < 16; ++i) x[i] = x[i] * a.sl2 + entry[acc_row(i, 0)];
                 }
             }
             if (j0 + 32 > lim_min) {
@@ -136,44 +121,10 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
                 for (int i = 0; i < 16; ++i)
                     if (j0 + acc_row(i, hh) >= lim) x[i] = -__builtin_inff();
             }
-            float p_sum = 0.f, ds_sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float p = __builtin_amdgcn_exp2f(BIAS ? x[i] - off : x[i] * a.sl2 - off);
-                dp[i] = p * (dp[i] - delta);
-                if (BIAS) {
-                    x[i] = p;
-                    p_sum += p;
-                    ds_sum += dp[i];
-                }
-            }
-            if (BIAS) {
-                sum_all += ds_sum;
-                if (behind) {
-                    sum_lo += ds_sum;
-                    p_lo += p_sum;
-                } else if (ahead) {
-                    sum_hi += ds_sum;
-                    p_hi += p_sum;
-                } else {
-                    // At the same time only lanes of one half: those of a head then add to different distances, so that the order of every
-                    // sum is that of the program (the LDS operations of a wavefront execute in order).
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int at_x = x0 + acc_row(i, hh);
-                        if (at_x <= 0) {
-                            sum_lo += dp[i];
-                            p_lo += x[i];
-                        } else if (at_x >= a.tab - 1) {
-                            sum_hi += dp[i];
-                            p_hi += x[i];
-                        } else {
-                            float *to = near + g * a.tab + at_x;
-                            if (hh == 0) lds_add(to, dp[i]);
-                            if (hh == 1) lds_add(to, dp[i]);
-                        }
-                    }
-                }
+                dp[i] = __builtin_amdgcn_exp2f(BIAS ? x[i] - off : x[i] * a.sl2 - off) * (dp[i] - delta);
+                miss += dp[i];
             }
             BFrag b[2];
             to_b_operand(dp, b);
@@ -197,39 +148,93 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
                     f32x4{dq[dt][4 * gq] * z, dq[dt][4 * gq + 1] * z, dq[dt][4 * gq + 2] * z, dq[dt][4 * gq + 3] * z};
             }
     }
-    if (BIAS && a.part_bias != nullptr) {
-        // D comes from outputs that were rounded: it is off by the sum of dS over all keys, which belongs to be zero.  The far
-        // buckets, sums over many keys that nearly cancel, are put right by it.
-        const float miss = half_sum(sum_all);
-        const float lo = half_sum(sum_lo) - miss * half_sum(p_lo), hi = half_sum(sum_hi) - miss * half_sum(p_hi);
-        if (hh == 0) {
-            far[wave * 64 + lane] = live ? lo : 0.f;
-            far[wave * 64 + 32 + lane] = live ? hi : 0.f;
+    // D was taken from outputs that are rounded, as are the probabilities they were summed with; it is off by the sum of dS over
+    // all keys, which belongs to be zero.  The other pass, and with it dK and the bias' gradient, get it put right.
+    miss = half_sum(miss);
+    if (live && hh == 0)
+        a.aux[((int64_t)part * a.h_q + head) * a.n_q + s.q0 + tok] = make_float2(off, -miss - (part == 0 ? delta : 0.f));
+}
+
+// Sums of dS by distance, of a tile of 32 queries and 32 keys: a wavefront writes the tile skewed, so that a distance's elements lie in one
+// row, each lane sums a row and adds it to the distance's place.  (Floating-point additions in LDS, one for each element, took 3.8 us
+// a tile; this takes 0.3.)  Places of a row that no element has stay zero from the start.
+// NE: elements of an accumulator at a time, 16 (the whole tile) or 4 (eight queries; at d = 128, where LDS is short).
+template <int NE>
+struct Skew {
+    static constexpr int ROWS = 2 * NE, TOP = NE == 16 ? 31 : 11;      // queries; distance of row 0 below that of the first query and key
+    static constexpr int N = 32 + TOP, PITCH = ROWS + 1;               // distances, floats from one to the next
+    static constexpr int BYTES = (N * PITCH * 4 + 15) / 16 * 16;
+};
+template <int NE>
+__device__ __forceinline__ void add_by_distance(const f32x16 &ds, bool live, float *skew, float *near, int lane) {
+    using S = Skew<NE>;
+    const int hh = lane >> 5, jl = lane & 31;
+#pragma unroll
+    for (int pass = 0; pass < 16 / NE; ++pass) {
+        const int first = NE == 16 ? 0 : 16 * (pass / 2) + 4 * (pass % 2);  // query of the pass' first element
+#pragma unroll
+        for (int m = 0; m < NE; ++m) {
+            const int e = pass * NE + m, row = acc_row(m, hh), place = NE == 16 ? row : m + 4 * hh;
+            skew[(jl - row + S::TOP) * S::PITCH + place] = live ? ds[e] : 0.f;
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        wg_barrier();
-        for (int i = threadIdx.x; i < a.group * a.n_buckets; i += 256) {
-            const int gi = i / a.n_buckets, b = i % a.n_buckets;
-            float sum = 0.f;
-            if (b > 0 && b < a.n_buckets - 1)
-                for (int w = 0; w < 4; ++w)
-                    for (int z = a.bounds[b - 1] - a.b0 + 1; z < a.bounds[b] - a.b0 + 1; ++z) sum += tab[(1 + w) * n_tab + gi * a.tab + z];
-            if (b == 0 || b == a.n_buckets - 1) {
-                // rows of this head: (row % group) == gi
-                for (int z = (gi + a.group - v_wg % a.group) % a.group; z < 128; z += a.group) {
-                    const float *f = far + (z / 32) * 64 + z % 32;
-                    if (b == 0) sum += f[0];
-                    if (b == a.n_buckets - 1) sum += f[32];
-                }
-            }
-            a.part_bias[((int64_t)slot * a.h_q + head_kv * a.group) * a.n_buckets + i] = sum;
+        // (lanes read what others wrote: the compiler, which sees one of them, must not move accesses across)
+        asm volatile("" ::: "memory");
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        if (lane < S::N) {
+#pragma unroll
+            for (int r = 0; r < S::ROWS; ++r) sum[r % 4] += skew[lane * S::PITCH + r];
+            near[lane - S::TOP - first] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         }
+        asm volatile("" ::: "memory");
     }
 }
 
+// What a workgroup has summed of the bias' gradient of one query head goes to its place, and the sums begin anew.
+// near: [4 wavefronts][a.tab] by distance; lo, hi: of the lane, tiles before the first and from the last bound on.
+__device__ __forceinline__ void flush_bias(const AttnArgs &a, float *near, float *far, float lo, float hi, float *dst) {
+    for (int x = 32; x > 0; x /= 2) {
+        lo += __shfl_xor(lo, x);
+        hi += __shfl_xor(hi, x);
+    }
+    if (threadIdx.x % 64 == 0) {
+        far[threadIdx.x / 64] = lo;
+        far[4 + threadIdx.x / 64] = hi;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    wg_barrier();
+    for (int x = threadIdx.x; x < a.tab; x += 256) {
+        near[x] = (near[x] + near[a.tab + x]) + (near[2 * a.tab + x] + near[3 * a.tab + x]);
+        near[a.tab + x] = near[2 * a.tab + x] = near[3 * a.tab + x] = 0.f;
+    }
+    __syncthreads();
+    // four threads to a bucket
+    const int b = threadIdx.x / 4, n = a.n_buckets;
+    float sum = 0.f;
+    if (b < n) {
+        const int from = b > 0 ? bias_entry(a, a.bounds[b - 1]) : 0, to = b < n - 1 ? bias_entry(a, a.bounds[b]) : a.tab;
+        for (int x = from + threadIdx.x % 4; x < to; x += 4) sum += near[x];
+    }
+    sum += __shfl_xor(sum, 1);
+    sum += __shfl_xor(sum, 2);
+    if (b == 0) sum += (far[0] + far[1]) + (far[2] + far[3]);
+    if (b == n - 1) sum += (far[4] + far[5]) + (far[6] + far[7]);
+    if (b < n && threadIdx.x % 4 == 0) dst[b] = sum;
+    __syncthreads();
+    for (int x = threadIdx.x; x < a.tab; x += 256) near[x] = 0.f;
+    __syncthreads();
+}
+
+// At d = 128 the value fragments of a wavefront's keys are read from LDS in every step, not held in 32 registers: with them two
+// wavefronts do not fit a SIMD.
+template <int D>
+constexpr int kSkew = D == 128 ? 4 : 16;
+template <int D>
+constexpr int kDkvValues = D == 128 ? 4 * AttnGeo<D>::TILE : 0;
+
 template <int D, bool BIAS>
-__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attn_dkv_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
     using G = AttnGeo<D>;
+    constexpr bool V_LDS = kDkvValues<D> > 0;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv, place = blockIdx.x / a.h_kv;
@@ -237,14 +242,23 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attn_dkv_kernel(AttnArg
     const int seq = find_sequence(a.k_off, a.n_k, a.n_seq, 1, 128, slot);
     const Sequence s = load_sequence(a, seq);
     const int j_wg = (slot - tile_slot(a.k_off, a.n_k, 1, 128, seq)) * 128;
-    if (j_wg < 0 || j_wg >= s.k_slot) return;
+    const bool none = j_wg < 0 || j_wg >= s.k_slot;
     const int j0 = j_wg + wave * 32, j = j0 + (lane & 31);
     const bool live = j < s.n_k;
     // query tiles of 32: those of a head from the first that sees a key of this workgroup on, head after head
     const int n_t = (s.n_q + 31) / 32, t0 = a.causal ? min(max(j_wg - s.shift, 0) / 32, n_t) : 0;
-    const int n_all = j_wg < s.n_k ? a.group * (n_t - t0) : 0, per = (n_all + a.parts - 1) / a.parts;
+    const int n_all = !none && j_wg < s.n_k ? a.group * (n_t - t0) : 0, per = (n_all + a.parts - 1) / a.parts;
     const int i_begin = part * per, i_end = min(i_begin + per, n_all);
-    bf16x8 kf[G::NS], vf[G::NS];
+    float *sums = BIAS && a.part_bias != nullptr ? a.part_bias + ((int64_t)place * a.h_q + head_kv * a.group) * a.n_buckets : nullptr;
+    if (BIAS && sums != nullptr) {  // heads that this part does not walk
+        const int g_first = i_begin < i_end ? i_begin / (n_t - t0) : a.group, g_last = i_begin < i_end ? (i_end - 1) / (n_t - t0) : -1;
+        for (int i = threadIdx.x; i < a.group * a.n_buckets; i += 256) {
+            const int g = i / a.n_buckets;
+            if (g < g_first || g > g_last) sums[i] = 0.f;
+        }
+    }
+    if (none) return;
+    bf16x8 kf[G::NS], vf[V_LDS ? 1 : G::NS];
     f32x16 dk[G::ND], dv[G::ND];
 #pragma unroll
     for (int dt = 0; dt < G::ND; ++dt)
@@ -253,57 +267,81 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attn_dkv_kernel(AttnArg
     if (i_begin < i_end) {
         const uint32_t q_row = (uint32_t)a.qs[0] * 2, o_row = (uint32_t)a.os[0] * 2;
         const CopyLane<D> c(lane);
+        constexpr int STEP = G::COPIES < 4 ? G::COPIES : 4, RING = kDkvRing<D>;
         auto copy_tile = [&](int i, int g, int qt) {
-            char *at = lds + ((i - i_begin) & 1) * kDkvSlot<D>;
+            char *at = lds + ((i - i_begin) & (RING - 1)) * kDkvSlot<D>;
             const int head = head_kv * a.group + g, avail = s.n_q - 32 * qt;
             const int64_t row = s.q0 + 32 * qt;
-            copy_rows<D, 32, 4 < G::COPIES ? 4 : G::COPIES>(reinterpret_cast<const char *>(a.q + row * a.qs[0] + head * a.qs[1]), q_row, avail, at,
-                                                            wave % G::COPIES, c);
-            copy_rows<D, 32, 4 < G::COPIES ? 4 : G::COPIES>(reinterpret_cast<const char *>(a.dout + row * a.os[0] + head * a.os[1]), o_row, avail,
-                                                            at + G::TILE, wave % G::COPIES, c);
+            copy_rows<D, 32, STEP>(reinterpret_cast<const char *>(a.q + row * a.qs[0] + head * a.qs[1]), q_row, avail, at, wave % STEP, c);
+            copy_rows<D, 32, STEP>(reinterpret_cast<const char *>(a.dout + row * a.os[0] + head * a.os[1]), o_row, avail, at + G::TILE,
+                                   wave % STEP, c);
             if (wave == 0)
                 copy_256_to_lds(a.aux + (int64_t)head * a.n_q + row, min(lane & 31, avail - 1) * 8 + hh * 4, at + 2 * G::TILE);
         };
-        int g = i_begin / (n_t - t0), qt = t0 + i_begin % (n_t - t0);
-        copy_tile(i_begin, g, qt);
-        float *tab = reinterpret_cast<float *>(lds + kDkvLds<D>);
-        if (BIAS) expand_bias(a, head_kv, tab, 256);
+        int g = i_begin / (n_t - t0), qt = t0 + i_begin % (n_t - t0), g_copy = g, qt_copy = qt, i_copy = i_begin;
+        auto copy_next = [&] {
+            copy_tile(i_copy, g_copy, qt_copy);
+            ++i_copy;
+            if (++qt_copy == n_t) {
+                qt_copy = t0;
+                ++g_copy;
+            }
+        };
+        for (int n = 0; n < RING - 1 && i_copy < i_end; ++n) copy_next();
+        char *values = lds + kDkvLds<D> + wave * G::TILE + lane * 16;  // of this lane: D / 16 pieces of 16 bytes, 1 KB apart
+        float *tab = reinterpret_cast<float *>(lds + kDkvLds<D> + kDkvValues<D>), *far = tab + a.group * a.tab, *near = far + 8;
+        float *skew = near + 4 * a.tab + wave * (Skew<kSkew<D>>::BYTES / 4);
+        float lo = 0.f, hi = 0.f;
+        if (BIAS) {
+            expand_bias(a, head_kv, tab, 256);
+            if (sums != nullptr)
+                for (int i = threadIdx.x; i < 4 * a.tab + Skew<kSkew<D>>::BYTES; i += 256) near[i] = 0.f;  // (and the four wavefronts' skews)
+        }
         const int jc = min(j, s.n_k - 1);
         const uint16_t *kp = a.k + (s.k0 + jc) * a.ks[0] + head_kv * a.ks[1] + 8 * hh;
         const uint16_t *vp = a.v + (s.k0 + jc) * a.vs[0] + head_kv * a.vs[1] + 8 * hh;
 #pragma unroll
         for (int ks = 0; ks < G::NS; ++ks) {
             kf[ks] = *reinterpret_cast<const bf16x8 *>(kp + 16 * ks);
-            vf[ks] = *reinterpret_cast<const bf16x8 *>(vp + 16 * ks);
+            if constexpr (V_LDS)
+                *reinterpret_cast<bf16x8 *>(values + ks * 1024) = *reinterpret_cast<const bf16x8 *>(vp + 16 * ks);
+            else
+                vf[ks] = *reinterpret_cast<const bf16x8 *>(vp + 16 * ks);
         }
         const TileLane<D> t(lane);
-        const int b_last = a.b0 + a.tab - 2;
         for (int i = i_begin; i < i_end; ++i) {
-            wait_copies<0>();
+            // the tiles behind this one may still be under way (two copy instructions each, with a third of the first wavefront's)
+            constexpr int PER = 2 * G::COPIES / STEP;
+            if (i_copy - i <= 1)
+                wait_copies<0>();
+            else if (wave == 0)
+                i_copy - i == 2 ? wait_copies<PER + 1>() : wait_copies<2 * (PER + 1)>();
+            else
+                i_copy - i == 2 ? wait_copies<PER>() : wait_copies<2 * PER>();
             wg_barrier();
+            if (i_copy < i_end) copy_next();
             int g_next = g, qt_next = qt + 1;
             if (qt_next == n_t) {
                 qt_next = t0;
                 ++g_next;
             }
-            if (i + 1 < i_end) copy_tile(i + 1, g_next, qt_next);
             const int p0 = 32 * qt + s.shift;  // position of the tile's first query
             if (j0 < s.n_k && !(a.causal && p0 + 31 < j0)) {
-                const char *at = lds + ((i - i_begin) & 1) * kDkvSlot<D>;
+                const char *at = lds + ((i - i_begin) & (RING - 1)) * kDkvSlot<D>;
                 const float *aux = reinterpret_cast<const float *>(at + 2 * G::TILE) + 8 * hh;
-                f32x16 x, dp;
-                mfma_rows<D>(x, at, t, kf);
-                mfma_rows<D>(dp, at + G::TILE, t, vf);
+                f32x16 p, dp;
+                mfma_rows<D>(p, at, t, kf);
+                const bool behind = BIAS && j0 + 31 - p0 < a.b0, ahead = BIAS && j0 - p0 - 31 >= a.b_last;
                 if (BIAS) {
                     const float *tab_g = tab + g * a.tab;
-                    if (j0 + 31 - p0 < a.b0 || j0 - p0 - 31 >= b_last) {
-                        const float b = tab_g[j0 - p0 - 31 >= b_last ? a.tab - 1 : 0];
+                    if (behind || ahead) {
+                        const float b = tab_g[ahead ? a.tab - 1 : 0];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) x[e] = x[e] * a.sl2 + b;
+                        for (int e = 0; e < 16; ++e) p[e] = p[e] * a.sl2 + b;
                     } else {
-                        const int x0 = j - p0 - a.b0 + 1;
+                        const float *entry = tab_g + bias_entry(a, j - p0) - 8 * hh;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) x[e] = x[e] * a.sl2 + tab_g[min(max(x0 - acc_row(e, hh), 0), a.tab - 1)];
+                        for (int e = 0; e < 16; ++e) p[e] = p[e] * a.sl2 + entry[-acc_row(e, 0)];
                     }
                 }
                 if (32 * qt + 32 > s.n_q || (a.causal && j0 + 31 > p0)) {
@@ -312,25 +350,50 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attn_dkv_kernel(AttnArg
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int row = acc_row(e, hh);
-                        if (row < from || row >= to) x[e] = -__builtin_inff();
+                        if (row < from || row >= to) p[e] = -__builtin_inff();
                     }
                 }
-                f32x16 p;
 #pragma unroll
                 for (int e4 = 0; e4 < 16; e4 += 4) {
                     const f32x4 off = *reinterpret_cast<const f32x4 *>(aux + 16 * (e4 / 8) + e4 % 8);
-                    const f32x4 nd = *reinterpret_cast<const f32x4 *>(aux + 32 + 16 * (e4 / 8) + e4 % 8);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        p[e4 + e] = __builtin_amdgcn_exp2f(BIAS ? x[e4 + e] - off[e] : x[e4 + e] * a.sl2 - off[e]);
-                        dp[e4 + e] = p[e4 + e] * (dp[e4 + e] + nd[e]);
-                    }
+                    for (int e = 0; e < 4; ++e) p[e4 + e] = __builtin_amdgcn_exp2f(BIAS ? p[e4 + e] - off[e] : p[e4 + e] * a.sl2 - off[e]);
                 }
                 BFrag b[2];
                 to_b_operand(p, b);
                 mfma_transposed<D>(dv, at + G::TILE, t, b);
+                if constexpr (V_LDS) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) dp[e] = 0.f;
+#pragma unroll
+                    for (int ks = 0; ks < G::NS; ++ks)
+                        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_row_frag<D>(at + G::TILE, t, ks),
+                                                                     *reinterpret_cast<const bf16x8 *>(values + ks * 1024), dp, 0, 0, 0);
+                } else {
+                    mfma_rows<D>(dp, at + G::TILE, t, vf);
+                }
+#pragma unroll
+                for (int e4 = 0; e4 < 16; e4 += 4) {
+                    const f32x4 nd = *reinterpret_cast<const f32x4 *>(aux + 32 + 16 * (e4 / 8) + e4 % 8);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dp[e4 + e] = p[e4 + e] * (dp[e4 + e] + nd[e]);
+                }
+                if (BIAS && sums != nullptr) {
+                    if (behind || ahead) {
+                        float sum = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) sum += live ? dp[e] : 0.f;
+                        if (behind) lo += sum; else hi += sum;
+                    } else {
+                        add_by_distance<kSkew<D>>(dp, live, skew, near + wave * a.tab + bias_entry(a, j0 - p0), lane);
+                    }
+                }
                 to_b_operand(dp, b);
                 mfma_transposed<D>(dk, at, t, b);
+            }
+            if (BIAS && sums != nullptr && (g_next != g || i + 1 == i_end)) {
+                flush_bias(a, near, far, lo, hi, sums + g * a.n_buckets);
+                lo = hi = 0.f;
             }
             g = g_next;
             qt = qt_next;
@@ -394,6 +457,12 @@ __global__ __launch_bounds__(256) void attn_sum_parts(AttnArgs a) {
     if (first < 0 || first >= rows) return;
     constexpr int CH = D / 8;
     const int64_t step = (int64_t)n * heads * D;
+    if (Q && threadIdx.x < 128 && first + (int)threadIdx.x < s.n_q) {
+        float2 *at = a.aux + (int64_t)head * n + row0 + first + threadIdx.x;
+        float2 x = at[0];
+        for (int p = 1; p < a.parts; ++p) x.y += at[(int64_t)p * heads * n].y;
+        at[0] = x;
+    }
     for (int which = 0; which < (Q ? 1 : 2); ++which) {
         const float *from = Q ? a.part_q : which == 0 ? a.part_k : a.part_v;
         uint16_t *dst = Q ? a.dq : which == 0 ? a.dk : a.dv;
@@ -414,16 +483,18 @@ __global__ __launch_bounds__(256) void attn_sum_parts(AttnArgs a) {
 }
 
 // The bias' gradient: what the workgroups of a head left, added in order (in 64 bits).
-__global__ __launch_bounds__(256) void attn_sum_bias(AttnArgs a) {
-    __shared__ double sums[4][kMaxBuckets];
+__global__ __launch_bounds__(1024) void attn_sum_bias(AttnArgs a) {
+    __shared__ double sums[16][kMaxBuckets];
     const int head = blockIdx.x, b = threadIdx.x % 64, way = threadIdx.x / 64;
     double x = 0.;
     if (b < a.n_buckets)
-        for (int i = way; i < a.n_slots; i += 4) x += a.part_bias[((int64_t)i * a.h_q + head) * a.n_buckets + b];
+#pragma unroll 4
+        for (int i = way; i < a.n_slots; i += 16) x += a.part_bias[((int64_t)i * a.h_q + head) * a.n_buckets + b];
     sums[way][b] = x;
     __syncthreads();
     if (way == 0 && b < a.n_buckets) {
-        const __bf16 y = (__bf16)(float)(sums[0][b] + sums[1][b] + sums[2][b] + sums[3][b]);
+        for (int i = 1; i < 16; ++i) x += sums[i][b];
+        const __bf16 y = (__bf16)(float)x;
         a.dbias[head * a.n_buckets + b] = *reinterpret_cast<const uint16_t *>(&y);
     }
 }
@@ -441,7 +512,7 @@ WsLayout layout(const AttnArgs &a, int d) {
     auto parts = [&](int64_t wgs, int64_t walk) {  // walk: tiles of 32 that an average workgroup walks
         return (int)std::min<int64_t>(std::max<int64_t>(512 / std::max<int64_t>(wgs, 1), 1), std::min<int64_t>(std::max<int64_t>(walk / 8, 1), 16));
     };
-    w.q_parts = a.n_buckets > 0 ? 1 : parts((rows / 128 + 1) * a.h_kv, (int64_t)a.n_k / a.n_seq / 32);
+    w.q_parts = parts((rows / 128 + 1) * a.h_kv, (int64_t)a.n_k / a.n_seq / 32);
     w.k_parts = parts(((int64_t)a.n_k / 128 + 1) * a.h_kv, rows / a.n_seq / 32);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -449,11 +520,11 @@ WsLayout layout(const AttnArgs &a, int d) {
         at += align_up(bytes, 256);
         return here;
     };
-    w.aux = take((size_t)a.n_q * a.h_q * 8);
+    w.aux = take((size_t)w.q_parts * a.n_q * a.h_q * 8);
     w.part_q = take(w.q_parts > 1 ? (size_t)w.q_parts * a.n_q * a.h_q * d * 4 : 0);
     w.part_k = take(w.k_parts > 1 ? (size_t)w.k_parts * a.n_k * a.h_kv * d * 4 : 0);
     w.part_v = take(w.k_parts > 1 ? (size_t)w.k_parts * a.n_k * a.h_kv * d * 4 : 0);
-    w.part_bias = take(a.n_buckets > 0 ? (size_t)w.q_slots * a.h_q * a.n_buckets * 4 : 0);
+    w.part_bias = take(a.n_buckets > 0 ? (size_t)w.k_slots * w.k_parts * a.h_q * a.n_buckets * 4 : 0);
     w.total = at;
     return w;
 }
@@ -473,18 +544,19 @@ lsrm_status launch_backward_d(AttnArgs a, void *ws, hipStream_t st) {
         a.n_slots = w.q_slots;
         a.parts = w.q_parts;
         lsrm_status rc = launch_attn(bias ? &attn_dq_kernel<D, true> : &attn_dq_kernel<D, false>, (int64_t)w.q_slots * a.h_kv * w.q_parts, 256,
-                                     kDqLds<D> + (bias ? 5 * n_tab + 1024 : 0), a, st);
+                                     kDqLds<D> + n_tab, a, st);
         if (rc != LSRM_OK) return rc;
         if (w.q_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, true>, (int64_t)(a.n_q / 128 + a.n_seq) * a.h_q, 256, 0, a, st)) != LSRM_OK) return rc;
         a.parts = w.k_parts;
         rc = launch_attn(bias ? &attn_dkv_kernel<D, true> : &attn_dkv_kernel<D, false>, (int64_t)w.k_slots * a.h_kv * w.k_parts, 256,
-                         kDkvLds<D> + n_tab, a, st);
+                         kDkvLds<D> + kDkvValues<D> + (bias ? n_tab + 32 + (a.dbias != nullptr ? 16 * a.tab + 4 * Skew<kSkew<D>>::BYTES : 0) : 0), a, st);
         if (rc != LSRM_OK) return rc;
+        a.n_slots = w.k_slots * w.k_parts;  // (of the bias' sums)
         if (w.k_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, false>, (int64_t)w.k_slots * a.h_kv, 256, 0, a, st)) != LSRM_OK) return rc;
     } else {
         a.n_slots = 0;
     }
-    if (bias && a.dbias != nullptr) return launch_attn(&attn_sum_bias, a.h_q, 256, 0, a, st);
+    if (bias && a.dbias != nullptr) return launch_attn(&attn_sum_bias, a.h_q, 1024, 0, a, st);
     return LSRM_OK;
 }
 

@@ -62,14 +62,15 @@ __device__ __forceinline__ void load_rows(const AttnArgs &a, const Sequence &s, 
 // Scores, with a bias, are kept in the exponent's unit (times log2e); without one the factor goes into the exponential's argument.
 template <int D, bool BIAS>
 __device__ __forceinline__ void add_bias(const AttnArgs &a, const Rows<D, BIAS> &r, f32x16 &s, int j0, int hh) {
-    if (j0 + 31 - r.pos_min < a.b0 || j0 - r.pos_max >= a.b0 + a.tab - 2) {  // one bucket for the whole tile
-        const float c = r.tab[j0 - r.pos_max >= a.b0 + a.tab - 2 ? a.tab - 1 : 0];
+    const bool ahead = j0 - r.pos_max >= a.b_last;
+    if (ahead || j0 + 31 - r.pos_min < a.b0) {  // one bucket for the whole tile
+        const float c = r.tab[ahead ? a.tab - 1 : 0];
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = s[i] * a.sl2 + c;
     } else {
-        const int x0 = j0 - r.pos - a.b0 + 1;
+        const float *at = r.tab + bias_entry(a, j0 - r.pos) + 8 * hh;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = s[i] * a.sl2 + r.tab[min(max(x0 + acc_row(i, hh), 0), a.tab - 1)];
+        for (int i = 0; i < 16; ++i) s[i] = s[i] * a.sl2 + at[acc_row(i, 0)];
     }
 }
 

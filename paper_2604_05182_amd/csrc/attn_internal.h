@@ -15,7 +15,9 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxBuckets = 64;
-constexpr int kMaxBiasEntries = 4096;  // of the expanded bias of a group of heads (in LDS: 16 KB, and four times that for its gradient)
+constexpr int kBiasPad = 64;             // entries on each side of a head's expanded bias that repeat its first and last one
+constexpr int kMaxBiasEntries = 10240;   // of the expanded bias of a group of heads, with the repeated ones (in LDS: 40 KB)
+constexpr int kMaxBiasSpan = 1022;       // last bound - first bound (the gradient's sums take up to 18 KB)
 
 struct AttnArgs {
     const uint16_t *q, *k, *v, *bias, *dout, *o;
@@ -29,9 +31,10 @@ struct AttnArgs {
     int unit_cap;          // forward of few rows: units of all sequences at most
     int parts;             // backward: parts that a walk is cut into
     float *part;           // forward of few rows: sums of the parts
-    float2 *aux;           // backward: [h_q][n_q] {lse log2e (+inf for a query without keys), -D}
+    float2 *aux;           // backward: [h_q][n_q] {lse log2e (+inf for a query without keys), -D}, one such for each part of the dQ walks
     float *part_q, *part_k, *part_v, *part_bias;
-    int n_buckets, b0, tab;  // tab: entries of a head's expanded bias (0: no bias), for distances b0 - 1 .. b0 + tab - 2
+    int n_buckets, b0, b_last;  // of the bias (0: none), first and last bound
+    int tab;                    // entries of a head's expanded bias
     int32_t bounds[kMaxBuckets - 1];
     float scale, sl2;
 };
@@ -298,8 +301,10 @@ lsrm_status launch_attn(F kernel, int64_t grid, int threads, int lds, const Attn
 }
 
 // ---- the bias --------------------------------------------------------------------------------------------------------
-// The bias of one key/value head's query heads, expanded by distance, times log2e: entry x of a head is for the distance b0 - 1 + x,
-// the first for everything before, the last for everything behind.  -1e30 and below mask their bucket.
+// The bias of one key/value head's query heads, expanded by distance, times log2e: entry x of a head is for the distance
+// b0 - 1 - kBiasPad + x.  What a tile of 32 queries and 32 keys looks up lies within the entries unless all its distances are before the first or
+// from the last bound on (then one bucket serves the tile): a lane's entries are at fixed places around one address, with no
+// clamping of single distances.  -1e30 and below mask their bucket.
 __device__ __forceinline__ int bucket_of(const AttnArgs &a, int rel) {
     int b = 0;
     for (int i = 0; i < a.n_buckets - 1; ++i) b += a.bounds[i] <= rel;
@@ -307,12 +312,14 @@ __device__ __forceinline__ int bucket_of(const AttnArgs &a, int rel) {
 }
 __device__ __forceinline__ void expand_bias(const AttnArgs &a, int head_kv, float *tab, int threads) {
     for (int x = threadIdx.x; x < a.tab; x += threads) {
-        const int b = bucket_of(a, a.b0 - 1 + x);
+        const int b = bucket_of(a, a.b0 - 1 - kBiasPad + x);
         for (int g = 0; g < a.group; ++g) {
             const float y = __uint_as_float((uint32_t)a.bias[(int64_t)(head_kv * a.group + g) * a.n_buckets + b] << 16);
             tab[g * a.tab + x] = y <= -1.0e30f ? -__builtin_inff() : y * kLog2e;
         }
     }
 }
+// entry of distance rel
+__device__ __forceinline__ int bias_entry(const AttnArgs &a, int rel) { return rel - a.b0 + 1 + kBiasPad; }
 
 }  // namespace lsrm

@@ -7,8 +7,9 @@ which covers scores of up to a few dozen with contractions over 128 channels, an
   out    u (sum_j P |v| + |out|)
   delta  D = dout . out is taken from rounded outputs: |dD| <= sum_c |dout_c| err(out_c)
   dv     u (sum_i P |dout| + |dv|)
-  dq     u (scale sum_j |dS| |k| + |dq|) + scale sum_j P |k| |dD|        (dk alike)
-  dbias  u |dbias| + sum P |dD| over the bucket's pairs
+  dq     u (scale sum_j |dS| |k| + |dq|) + scale sum_j P |k| |dD|
+  dk     u (scale sum_i |dS| |q| + |dk|)      (D is put right before dk and dbias use it: off by F's share only)
+  dbias  u |dbias|
 """
 import numpy as np
 import torch
@@ -80,19 +81,19 @@ def attention(q, k, v, q_rows, k_rows, causal=False, scale=0.0, bias=None, bound
             d_err = (np.abs(g) * out_err).sum(1, keepdims=True) + F * (np.abs(g) * np.abs(out)).sum(1, keepdims=True)
             ds = p * (dp - delta)
             mag = p * (np.abs(g) @ np.abs(vh).T + np.abs(delta))
-            ds_err = p * d_err + f * mag
+            ds_err, fine = p * d_err + f * mag, f * mag
             ads = np.abs(ds) + ds_err
             kv = t // (h // hk)
             val["dq"][a:a + lq, t] = sc * ds @ kh
             err["dq"][a:a + lq, t] = sc * (U * ads + ds_err) @ np.abs(kh) + U * np.abs(val["dq"][a:a + lq, t])
             val["dk"][b:b + lk, kv] += sc * ds.T @ qh
-            err["dk"][b:b + lk, kv] += sc * (U * ads + ds_err).T @ np.abs(qh)
+            err["dk"][b:b + lk, kv] += sc * (U * np.abs(ds) + (1 + U) * fine).T @ np.abs(qh)
             val["dv"][b:b + lk, kv] += p.T @ g
             err["dv"][b:b + lk, kv] += ((U + f) * p).T @ np.abs(g)
             if bias is not None:
                 n = bias.shape[1]
                 val["dbias"][t] += np.bincount(which.ravel(), ds.ravel(), minlength=n)
-                err["dbias"][t] += np.bincount(which.ravel(), ds_err.ravel(), minlength=n)
+                err["dbias"][t] += np.bincount(which.ravel(), fine.ravel(), minlength=n)
     if dout is not None:
         for x in ("dk", "dv", "dbias"):
             if x in val:

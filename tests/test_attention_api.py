@@ -48,7 +48,7 @@ def bad_params():
         (params(o_stride=((1 << 24) + 8, 64)), inv),
         (params(d=96), uns), (params(n_q=1 << 31, n_k=1 << 31), uns), (params(n_q=1 << 29, n_k=1 << 29, h_q=8), uns),
         (params(n_seq=1 << 24), uns), (params(bounds=list(range(64))), uns), (params(bounds=[0, (1 << 20) + 1]), uns),
-        (params(bounds=[-(1 << 20) - 1]), uns), (params(bounds=[0, 2047]), uns),
+        (params(bounds=[-(1 << 20) - 1]), uns), (params(bounds=[0, 1023]), uns), (params(h_q=16, h_kv=1, bounds=[0, 511], n_q=90, n_k=90), uns),
     ]
 
 
@@ -206,7 +206,9 @@ def test_bounds_let_rounding_pass_and_mistakes_fail():
         out = bf(bf(p) @ v[:, h])
         ds = p * (g[:, h] @ v[:, h].T - (g[:, h] * out).sum(1, keepdims=True))
         got["out"][:, h], got["lse"][:, h] = out, lse
-        got["dq"][:, h], got["dk"][:, h] = bf(bf(ds) @ k[:, h] / np.sqrt(32)), bf(bf(ds).T @ q[:, h] / np.sqrt(32))
+        got["dq"][:, h] = bf(bf(ds) @ k[:, h] / np.sqrt(32))
+        ds -= p * ds.sum(1, keepdims=True)
+        got["dk"][:, h] = bf(bf(ds).T @ q[:, h] / np.sqrt(32))
         got["dv"][:, h], got["dbias"][h] = bf(bf(p).T @ g[:, h]), bf(np.bincount(which.ravel(), ds.ravel(), minlength=3))
     for name in val:
         R.check(name, got[name], val[name], err[name])
