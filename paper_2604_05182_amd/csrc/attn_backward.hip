@@ -34,14 +34,14 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     const int head_kv = blockIdx.x % a.h_kv, place = blockIdx.x / a.h_kv;
     const int part = place % a.parts;
     const int slot = a.causal ? a.n_slots - 1 - place / a.parts : place / a.parts;
-    const int seq = find_sequence(a.q_off, a.n_q, a.n_seq, a.group, 128, slot);
-    const Sequence s = load_sequence(a, seq);
-    const int v_wg = (slot - tile_slot(a.q_off, a.n_q, a.group, 128, seq)) * 128, slot_rows = s.q_slot * a.group;
+    int tile;
+    const Sequence s = find_tile<false>(a, a.group, 128, slot, &tile);
+    const int v_wg = tile * 128, slot_rows = s.q_slot * a.group;
     const int n_rows = s.n_q * a.group;
     if (v_wg < 0 || v_wg >= slot_rows) return;
     auto seen = [&](int pos) { return a.causal ? min(max(pos + 1, 0), s.n_k) : s.n_k; };
-    const int keys = v_wg < n_rows ? seen(min(v_wg + 127, n_rows - 1) / a.group + s.shift) : 0;
-    const int st_all = (keys + kStage - 1) / kStage, st_per = (st_all + a.parts - 1) / a.parts;
+    const int keys = v_wg < n_rows ? seen(uniform((unsigned)min(v_wg + 127, n_rows - 1) / (unsigned)a.group) + s.shift) : 0;
+    const int st_all = (keys + kStage - 1) / kStage, st_per = uniform((st_all + a.parts - 1) / a.parts);
     const int st_begin = part * st_per, st_end = min(st_begin + st_per, st_all);
     const char *kb = reinterpret_cast<const char *>(a.k + s.k0 * a.ks[0] + head_kv * a.ks[1]);
     const char *vb = reinterpret_cast<const char *>(a.v + s.k0 * a.vs[0] + head_kv * a.vs[1]);
@@ -61,7 +61,8 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     const bool live = v < n_rows;
     const int last = max(min(v0 + 31, n_rows - 1), 0), vc = min(v, last);  // rows behind the last one do its work again, with P = 0
     const int tok = (unsigned)vc / (unsigned)a.group, g = vc - tok * a.group, head = head_kv * a.group + g;
-    const int pos = tok + s.shift, pos_min = v0 / a.group + s.shift, pos_max = last / a.group + s.shift;
+    const int pos = tok + s.shift, pos_min = uniform((unsigned)v0 / (unsigned)a.group) + s.shift;
+    const int pos_max = uniform((unsigned)last / (unsigned)a.group) + s.shift;
     const int lim = seen(pos), lim_min = seen(pos_min), lim_max = v0 < n_rows ? seen(pos_max) : 0;
     bf16x8 q[G::NS], dout[G::NS];
     float off = __builtin_inff(), delta = 0.f;
@@ -239,15 +240,15 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv, place = blockIdx.x / a.h_kv;
     const int part = place % a.parts, slot = place / a.parts;
-    const int seq = find_sequence(a.k_off, a.n_k, a.n_seq, 1, 128, slot);
-    const Sequence s = load_sequence(a, seq);
-    const int j_wg = (slot - tile_slot(a.k_off, a.n_k, 1, 128, seq)) * 128;
+    int tile;
+    const Sequence s = find_tile<true>(a, 1, 128, slot, &tile);
+    const int j_wg = tile * 128;
     const bool none = j_wg < 0 || j_wg >= s.k_slot;
     const int j0 = j_wg + wave * 32, j = j0 + (lane & 31);
     const bool live = j < s.n_k;
     // query tiles of 32: those of a head from the first that sees a key of this workgroup on, head after head
     const int n_t = (s.n_q + 31) / 32, t0 = a.causal ? min(max(j_wg - s.shift, 0) / 32, n_t) : 0;
-    const int n_all = !none && j_wg < s.n_k ? a.group * (n_t - t0) : 0, per = (n_all + a.parts - 1) / a.parts;
+    const int n_all = !none && j_wg < s.n_k ? a.group * (n_t - t0) : 0, per = uniform((n_all + a.parts - 1) / a.parts);
     const int i_begin = part * per, i_end = min(i_begin + per, n_all);
     float *sums = BIAS && a.part_bias != nullptr ? a.part_bias + ((int64_t)place * a.h_q + head_kv * a.group) * a.n_buckets : nullptr;
     if (BIAS && sums != nullptr) {  // heads that this part does not walk
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
             if (wave == 0)
                 copy_256_to_lds(a.aux + (int64_t)head * a.n_q + row, min(lane & 31, avail - 1) * 8 + hh * 4, at + 2 * G::TILE);
         };
-        int g = i_begin / (n_t - t0), qt = t0 + i_begin % (n_t - t0), g_copy = g, qt_copy = qt, i_copy = i_begin;
+        int g = uniform(i_begin / (n_t - t0)), qt = t0 + uniform(i_begin % (n_t - t0)), g_copy = g, qt_copy = qt, i_copy = i_begin;
         auto copy_next = [&] {
             copy_tile(i_copy, g_copy, qt_copy);
             ++i_copy;
@@ -289,7 +290,9 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
         };
         for (int n = 0; n < RING - 1 && i_copy < i_end; ++n) copy_next();
         char *values = lds + kDkvLds<D> + wave * G::TILE + lane * 16;  // of this lane: D / 16 pieces of 16 bytes, 1 KB apart
-        float *tab = reinterpret_cast<float *>(lds + kDkvLds<D> + kDkvValues<D>), *far = tab + a.group * a.tab, *near = far + 8;
+        // the bias, and of its gradient: sums of the wavefronts' far tiles, sums by distance, skewed tiles
+        float *tab = reinterpret_cast<float *>(lds + kDkvLds<D> + kDkvValues<D>), *far = tab + a.group * (a.tab + a.n_buckets) + kMaxBuckets;
+        float *near = far + 8;
         float *skew = near + 4 * a.tab + wave * (Skew<kSkew<D>>::BYTES / 4);
         float lo = 0.f, hi = 0.f;
         if (BIAS) {
@@ -449,11 +452,10 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
 template <int D, bool Q>
 __global__ __launch_bounds__(256) void attn_sum_parts(AttnArgs a) {
     const int heads = Q ? a.h_q : a.h_kv, n = Q ? a.n_q : a.n_k;
-    const int32_t *offs = Q ? a.q_off : a.k_off;
     const int head = blockIdx.x % heads, slot = blockIdx.x / heads;
-    const int seq = find_sequence(offs, n, a.n_seq, 1, 128, slot);
-    const Sequence s = load_sequence(a, seq);
-    const int first = (slot - tile_slot(offs, n, 1, 128, seq)) * 128, rows = Q ? s.q_slot : s.k_slot, row0 = Q ? s.q0 : s.k0;
+    int tile;
+    const Sequence s = find_tile<!Q>(a, 1, 128, slot, &tile);
+    const int first = tile * 128, rows = Q ? s.q_slot : s.k_slot, row0 = Q ? s.q0 : s.k0;
     if (first < 0 || first >= rows) return;
     constexpr int CH = D / 8;
     const int64_t step = (int64_t)n * heads * D;
@@ -540,7 +542,7 @@ lsrm_status launch_backward_d(AttnArgs a, void *ws, hipStream_t st) {
         a.part_k = reinterpret_cast<float *>(base + w.part_k);
         a.part_v = reinterpret_cast<float *>(base + w.part_v);
         a.part_bias = a.dbias != nullptr ? reinterpret_cast<float *>(base + w.part_bias) : nullptr;
-        const int n_tab = bias ? a.group * a.tab * 4 : 0;
+        const int n_tab = bias_lds_floats(a) * 4;
         a.n_slots = w.q_slots;
         a.parts = w.q_parts;
         lsrm_status rc = launch_attn(bias ? &attn_dq_kernel<D, true> : &attn_dq_kernel<D, false>, (int64_t)w.q_slots * a.h_kv * w.q_parts, 256,

@@ -47,8 +47,8 @@ __device__ __forceinline__ void load_rows(const AttnArgs &a, const Sequence &s, 
     const int last = min(v0 + 31, n_rows - 1), v = min(v0 + (lane & 31), last);
     const int tok = (unsigned)v / (unsigned)a.group, g = v - tok * a.group;
     r.pos = tok + s.shift;
-    r.pos_min = v0 / a.group + s.shift;
-    r.pos_max = last / a.group + s.shift;
+    r.pos_min = uniform((unsigned)v0 / (unsigned)a.group) + s.shift;
+    r.pos_max = uniform((unsigned)last / (unsigned)a.group) + s.shift;
     auto seen = [&](int pos) { return a.causal ? min(max(pos + 1, 0), s.n_k) : s.n_k; };
     r.lim = seen(r.pos);
     r.lim_min = seen(r.pos_min);
@@ -132,14 +132,14 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv;
     const int slot = a.causal ? a.n_slots - 1 - (int)(blockIdx.x / a.h_kv) : (int)(blockIdx.x / a.h_kv);
-    const int seq = find_sequence(a.q_off, a.n_q, a.n_seq, a.group, 128, slot);
-    const Sequence s = load_sequence(a, seq);
-    const int v0 = (slot - tile_slot(a.q_off, a.n_q, a.group, 128, seq)) * 128, slot_rows = s.q_slot * a.group;
+    int tile;
+    const Sequence s = find_tile<false>(a, a.group, 128, slot, &tile);
+    const int v0 = tile * 128, slot_rows = s.q_slot * a.group;
     if (v0 < 0 || v0 >= slot_rows) return;
     const int n_rows = s.n_q * a.group;
     int keys = 0;  // that the last live row sees, hence any
     if (v0 < n_rows) {
-        const int last = min(v0 + 127, n_rows - 1) / a.group;
+        const int last = uniform((unsigned)min(v0 + 127, n_rows - 1) / (unsigned)a.group);
         keys = a.causal ? min(max(last + s.shift + 1, 0), s.n_k) : s.n_k;
     }
     const int n_st = (keys + kStage - 1) / kStage;
@@ -245,14 +245,15 @@ __device__ __forceinline__ int unit_sequence(const AttnArgs &a, int unit, int ch
     return a.n_seq;
 }
 
-// Wavefronts of a workgroup.  Each has a ring of two slots (a K and a V tile) of its own; two workgroups share a CU at d = 128 too, so that
-// one streams while the other starts or ends.
-template <int D>
-constexpr int kFewWaves = D == 128 ? 2 : 4;
+// Wavefronts of a workgroup.  Each has a ring of two slots (a K and a V tile) of its own.  Where the keys are cut, two workgroups share a CU, so
+// that one streams while the other starts or ends; where they are not, a tile's keys are dealt to as many wavefronts as LDS has room for
+// (beside the largest expanded bias: half as many).
+template <int D, bool CROWDED>
+constexpr int kFewWaves = (D == 128 ? 2 : 4) * (CROWDED ? 1 : 2);
 template <int D>
 constexpr int kFewRing = 2 * 2 * AttnGeo<D>::TILE;  // per wavefront
-template <int D>
-constexpr int kFewLds = kFewWaves<D> * (kFewRing<D> + 256);
+template <int D, bool CROWDED>
+constexpr int kFewLds = kFewWaves<D, CROWDED> * (kFewRing<D> + 256);
 template <int D>
 constexpr int kPartFloats = kFewRows * (D + 2);
 
@@ -276,33 +277,31 @@ __device__ __forceinline__ void store_channels(const AttnArgs &a, const Sequence
 }
 
 template <int D, bool BIAS, bool SPLIT>
-__global__ __launch_bounds__(64 * kFewWaves<D>, 1) void attn_few_kernel(AttnArgs a) {
+__global__ __launch_bounds__((64 * kFewWaves<D, SPLIT || BIAS>), 1) void attn_few_kernel(AttnArgs a) {
     using G = AttnGeo<D>;
-    constexpr int NW = kFewWaves<D>, STEP = 32 * NW;
+    constexpr int NW = kFewWaves<D, SPLIT || BIAS>, STEP = 32 * NW;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv, unit = blockIdx.x / a.h_kv;
-    int seq, tile, part = 0, n_parts = 1, chunk = 0;
+    int tile, part = 0, n_parts = 1, chunk = 0;
+    Sequence s;
     if (SPLIT) {
         chunk = part_keys(a);
-        int within;
-        seq = unit_sequence(a, unit, chunk, &within);
+        const int seq = uniform(unit_sequence(a, unit, chunk, &tile));
         if (seq >= a.n_seq) return;
-        tile = within;
+        s = load_sequence(a, seq);
     } else {
-        seq = find_sequence(a.q_off, a.n_q, a.n_seq, a.group, kFewRows, unit);
-        tile = unit - tile_slot(a.q_off, a.n_q, a.group, kFewRows, seq);
+        s = find_tile<false>(a, a.group, kFewRows, unit, &tile);
     }
-    const Sequence s = load_sequence(a, seq);
     if (SPLIT) {
-        n_parts = parts_of(s, chunk);
-        part = tile % n_parts;
-        tile /= n_parts;
+        n_parts = uniform(parts_of(s, chunk));
+        part = uniform(tile % n_parts);
+        tile = uniform(tile / n_parts);
     }
     const int v0 = tile * kFewRows, slot_rows = s.q_slot * a.group;
     if (v0 < 0 || v0 >= slot_rows) return;
     Rows<D, BIAS> r;
-    float *tab = reinterpret_cast<float *>(lds + kFewLds<D>);
+    float *tab = reinterpret_cast<float *>(lds + kFewLds<D, SPLIT || BIAS>);
     load_rows<D, BIAS>(a, s, head_kv, v0, lane, tab, r);
     const int j_begin = SPLIT ? part * chunk : 0, j_end = min(SPLIT ? j_begin + chunk : s.n_k, r.lim_max);
     const char *kb = reinterpret_cast<const char *>(a.k + s.k0 * a.ks[0] + head_kv * a.ks[1]);
@@ -351,9 +350,9 @@ __global__ __launch_bounds__(64 * kFewWaves<D>, 1) void attn_few_kernel(AttnArgs
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     wg_barrier();
-    constexpr int TPR = 2 * NW, CH = D / TPR;  // threads per row, channels per thread
+    constexpr int TPR = 2 * NW < D / 4 ? 2 * NW : D / 4, CH = D / TPR;  // threads per row, channels per thread
     const int row = threadIdx.x / TPR, c0 = (threadIdx.x % TPR) * CH;
-    if (v0 + row >= slot_rows) return;
+    if (row >= kFewRows || v0 + row >= slot_rows) return;
     float m2 = ml[row], sum = 0.f, x[CH] = {};
 #pragma unroll
     for (int w = 1; w < NW; ++w) m2 = fmaxf(m2, ml[w * 64 + row]);
@@ -387,9 +386,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
     __shared__ f32x4 sums[GROUPS][LANES];
     __shared__ float part_max[4], part_sum[4];
     const int way = blockIdx.x % kJoinWays, head_kv = blockIdx.x / kJoinWays % a.h_kv, slot = blockIdx.x / kJoinWays / a.h_kv;
-    const int seq = find_sequence(a.q_off, a.n_q, a.n_seq, a.group, kFewRows, slot);
-    const int tile = slot - tile_slot(a.q_off, a.n_q, a.group, kFewRows, seq);
-    const Sequence s = load_sequence(a, seq);
+    int tile, seq;
+    const Sequence s = find_tile<false>(a, a.group, kFewRows, slot, &tile, &seq);
     const int slot_rows = s.q_slot * a.group;
     if (tile < 0 || tile * kFewRows + way >= slot_rows) return;
     const int chunk = part_keys(a), n_parts = parts_of(s, chunk);
@@ -442,20 +440,21 @@ template <int D>
 lsrm_status launch_forward_d(AttnArgs a, void *ws, hipStream_t st) {
     int64_t slots32;
     const Way way = forward_way(a, &slots32);
-    const int tab = a.n_buckets > 0 ? a.group * a.tab * 4 : 0;
+    const int tab = bias_lds_floats(a) * 4;
     const bool bias = a.n_buckets > 0;
     if (way == MANY) {
         a.n_slots = (int)((int64_t)a.n_q * a.group / 128 + a.n_seq);
         return launch_attn(bias ? &attn_forward_kernel<D, true> : &attn_forward_kernel<D, false>, (int64_t)a.n_slots * a.h_kv, 256,
                            kForwardLds<D> + tab, a, st);
     }
+    const int64_t n_tiles = slots32 * a.h_kv;
     if (way == FEW)
-        return launch_attn(bias ? &attn_few_kernel<D, true, false> : &attn_few_kernel<D, false, false>, slots32 * a.h_kv, 64 * kFewWaves<D>,
-                           kFewLds<D> + tab, a, st);
+        return bias ? launch_attn(&attn_few_kernel<D, true, false>, n_tiles, 64 * kFewWaves<D, true>, kFewLds<D, true> + tab, a, st)
+                    : launch_attn(&attn_few_kernel<D, false, false>, n_tiles, 64 * kFewWaves<D, false>, kFewLds<D, false>, a, st);
     a.unit_cap = unit_cap(a, slots32);
     a.part = static_cast<float *>(ws);
     lsrm_status rc = launch_attn(bias ? &attn_few_kernel<D, true, true> : &attn_few_kernel<D, false, true>, (int64_t)a.unit_cap * a.h_kv,
-                                 64 * kFewWaves<D>, kFewLds<D> + tab, a, st);
+                                 64 * kFewWaves<D, true>, kFewLds<D, true> + tab, a, st);
     if (rc != LSRM_OK) return rc;
     return launch_attn(&attn_join_kernel<D>, slots32 * a.h_kv * kJoinWays, 256, 0, a, st);
 }

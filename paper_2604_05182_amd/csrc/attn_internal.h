@@ -27,7 +27,7 @@ struct AttnArgs {
     const int32_t *q_off, *k_off, *q_len, *k_len;
     int64_t qs[2], ks[2], vs[2], os[2];  // {row, head} strides in elements
     int n_q, n_k, n_seq, h_q, h_kv, group, causal;
-    int n_slots;           // row tiles of all sequences at most (see find_sequence)
+    int n_slots;           // row tiles of all sequences at most (see find_tile)
     int unit_cap;          // forward of few rows: units of all sequences at most
     int parts;             // backward: parts that a walk is cut into
     float *part;           // forward of few rows: sums of the parts
@@ -46,6 +46,10 @@ size_t attn_backward_ws_bytes(const AttnArgs &a, int d);
 lsrm_status launch_attn_forward(AttnArgs a, int d, void *ws, hipStream_t st);
 lsrm_status launch_attn_backward(AttnArgs a, int d, void *ws, hipStream_t st);
 
+// A value that all lanes hold, as a scalar.  (Divisions are done by the vector unit, whose results the compiler takes for each lane's own: branches on
+// them then mask lanes, and addresses for the copies to LDS must be scalars.)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // ---- where a workgroup's rows are ------------------------------------------------------------------------------------
 // The query rows of a key/value head are numbered (query, head of its group), heads fastest: a tile of rows then reads a key or
 // value once for all heads that share it, single queries fill a tile with their heads, and a causal tile's rows see almost
@@ -56,35 +60,55 @@ struct Sequence {
     int shift;  // position of query 0
 };
 // (whatever the offsets and lengths hold, the rows lie in the tensors)
-__device__ __forceinline__ Sequence load_sequence(const AttnArgs &a, int s) {
+__device__ __forceinline__ Sequence sequence_of(const AttnArgs &a, int q0, int q1, int k0, int k1, int q_len, int k_len) {
     Sequence r;
-    r.q0 = min(max(a.q_off[s], 0), a.n_q);
-    r.q_slot = min(max(a.q_off[s + 1], r.q0), a.n_q) - r.q0;
-    r.k0 = min(max(a.k_off[s], 0), a.n_k);
-    r.k_slot = min(max(a.k_off[s + 1], r.k0), a.n_k) - r.k0;
-    r.n_q = a.q_len != nullptr ? min(max(a.q_len[s], 0), r.q_slot) : r.q_slot;
-    r.n_k = a.k_len != nullptr ? min(max(a.k_len[s], 0), r.k_slot) : r.k_slot;
+    r.q0 = min(max(q0, 0), a.n_q);
+    r.q_slot = min(max(q1, r.q0), a.n_q) - r.q0;
+    r.k0 = min(max(k0, 0), a.n_k);
+    r.k_slot = min(max(k1, r.k0), a.n_k) - r.k0;
+    r.n_q = a.q_len != nullptr ? min(max(q_len, 0), r.q_slot) : r.q_slot;
+    r.n_k = a.k_len != nullptr ? min(max(k_len, 0), r.k_slot) : r.k_slot;
     r.shift = r.n_k - r.n_q;
     return r;
 }
+__device__ __forceinline__ Sequence load_sequence(const AttnArgs &a, int s) {
+    return sequence_of(a, a.q_off[s], a.q_off[s + 1], a.k_off[s], a.k_off[s + 1], a.q_len != nullptr ? a.q_len[s] : 0,
+                       a.k_len != nullptr ? a.k_len[s] : 0);
+}
 
 // Tiles of `bm` rows have slots of their own without anyone counting them: sequence s starts at slot floor(first row / bm) + s, and has
-// at most as many tiles as there are slots up to the next one's start.  Returns the last sequence that starts at or before slot x:
-// a wavefront probes 64 places at a time (one round up to 64 sequences, two up to 4096).
-__device__ __forceinline__ int tile_slot(const int32_t *off, int n_rows, int mult, int bm, int s) {
-    return min(max(off[s], 0), n_rows) * mult / bm + s;
-}
-__device__ __forceinline__ int find_sequence(const int32_t *off, int n_rows, int n_seq, int mult, int bm, int x) {
-    const int lane = threadIdx.x & 63;
-    int lo = 0, hi = n_seq;
+// at most as many tiles as there are slots up to the next one's start.  find_tile returns the last sequence that starts at or before
+// slot x, and the number of the tile there (which may be none of its tiles): a wavefront probes 64 places at a time.  Up to 64 sequences each lane
+// loads one of them whole, so that there is one trip to memory, not two (0.7 us of every small kernel); two rounds of probes up to 4096.
+__device__ __forceinline__ int tile_slot(int off, int n_rows, int mult, int bm, int s) { return min(max(off, 0), n_rows) * mult / bm + s; }
+template <bool KEYS>
+__device__ __forceinline__ Sequence find_tile(const AttnArgs &a, int mult, int bm, int x, int *tile, int *seq = nullptr) {
+    const int lane = threadIdx.x & 63, n_rows = KEYS ? a.n_k : a.n_q;
+    const int32_t *off = KEYS ? a.k_off : a.q_off;
+    if (a.n_seq <= 64) {
+        const int i = min(lane, a.n_seq - 1);
+        const int q0 = a.q_off[i], q1 = a.q_off[i + 1], k0 = a.k_off[i], k1 = a.k_off[i + 1];
+        const int q_len = a.q_len != nullptr ? a.q_len[i] : 0, k_len = a.k_len != nullptr ? a.k_len[i] : 0;
+        const int start = tile_slot(KEYS ? k0 : q0, n_rows, mult, bm, i);
+        const uint64_t after = ~__builtin_amdgcn_ballot_w64(lane < a.n_seq && start <= x);
+        const int at = max(after == 0 ? 63 : (int)__builtin_ctzll(after) - 1, 0);
+        *tile = x - __builtin_amdgcn_readlane(start, at);
+        if (seq != nullptr) *seq = at;
+        return sequence_of(a, __builtin_amdgcn_readlane(q0, at), __builtin_amdgcn_readlane(q1, at), __builtin_amdgcn_readlane(k0, at),
+                           __builtin_amdgcn_readlane(k1, at), __builtin_amdgcn_readlane(q_len, at), __builtin_amdgcn_readlane(k_len, at));
+    }
+    int lo = 0, hi = a.n_seq;
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) / 64, s = lo + (lane + 1) * step;
-        const uint64_t below = __builtin_amdgcn_ballot_w64(s < hi && tile_slot(off, n_rows, mult, bm, s) <= x);
+        const uint64_t below = __builtin_amdgcn_ballot_w64(s < hi && tile_slot(off[min(s, a.n_seq - 1)], n_rows, mult, bm, s) <= x);
         const int c = __builtin_ctzll(~below);  // (the last lane's place is never below hi)
         lo += c * step;
         hi = min(hi, lo + step);
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    *tile = x - tile_slot(off[lo], n_rows, mult, bm, lo);
+    if (seq != nullptr) *seq = lo;
+    return load_sequence(a, lo);
 }
 
 // ---- tiles in LDS ----------------------------------------------------------------------------------------------------
@@ -129,6 +153,7 @@ template <int D, int N, int STEP>
 __device__ __forceinline__ void copy_rows(const char *src, uint32_t stride_b, int avail, const char *dst, int first, const CopyLane<D> &c) {
     using G = AttnGeo<D>;
     constexpr int N_COPY = N / G::RPC;
+    avail = uniform(avail);
     if (avail >= N) {
 #pragma unroll
         for (int n = 0; n < N_COPY / STEP; ++n) {
@@ -305,18 +330,26 @@ lsrm_status launch_attn(F kernel, int64_t grid, int threads, int lds, const Attn
 // b0 - 1 - kBiasPad + x.  What a tile of 32 queries and 32 keys looks up lies within the entries unless all its distances are before the first or
 // from the last bound on (then one bucket serves the tile): a lane's entries are at fixed places around one address, with no
 // clamping of single distances.  -1e30 and below mask their bucket.
-__device__ __forceinline__ int bucket_of(const AttnArgs &a, int rel) {
-    int b = 0;
-    for (int i = 0; i < a.n_buckets - 1; ++i) b += a.bounds[i] <= rel;
-    return b;
-}
+// In LDS behind the expanded entries: the bounds and the group's bias as it is.  Every thread of the workgroup takes part; nobody may read
+// before the next barrier.
+inline int bias_lds_floats(const AttnArgs &a) { return a.n_buckets > 0 ? a.group * a.tab + kMaxBuckets + a.group * a.n_buckets : 0; }
 __device__ __forceinline__ void expand_bias(const AttnArgs &a, int head_kv, float *tab, int threads) {
-    for (int x = threadIdx.x; x < a.tab; x += threads) {
-        const int b = bucket_of(a, a.b0 - 1 - kBiasPad + x);
-        for (int g = 0; g < a.group; ++g) {
-            const float y = __uint_as_float((uint32_t)a.bias[(int64_t)(head_kv * a.group + g) * a.n_buckets + b] << 16);
-            tab[g * a.tab + x] = y <= -1.0e30f ? -__builtin_inff() : y * kLog2e;
-        }
+    int *bounds = reinterpret_cast<int *>(tab + a.group * a.tab);
+    float *bias = tab + a.group * a.tab + kMaxBuckets;
+    const int tid = threadIdx.x, n = a.n_buckets;
+    if (tid < kMaxBuckets) bounds[tid] = tid < n - 1 ? a.bounds[tid] : 0x7fffffff;
+    for (int i = tid; i < a.group * n; i += threads) {
+        const float y = __uint_as_float((uint32_t)a.bias[(int64_t)head_kv * a.group * n + i] << 16);
+        bias[i] = y <= -1.0e30f ? -__builtin_inff() : y * kLog2e;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    wg_barrier();
+    for (int x = tid; x < a.tab; x += threads) {
+        const int rel = a.b0 - 1 - kBiasPad + x;
+        int b = 0;  // bounds that are <= rel
+#pragma unroll
+        for (int step = kMaxBuckets / 2; step > 0; step /= 2) b += bounds[b + step - 1] <= rel ? step : 0;
+        for (int g = 0; g < a.group; ++g) tab[g * a.tab + x] = bias[g * n + b];
     }
 }
 // entry of distance rel
