@@ -74,25 +74,46 @@ __device__ __forceinline__ void add_bias(const AttnArgs &a, const Rows<D, BIAS> 
     }
 }
 
-// One tile of 32 keys from key j0 of the sequence on.
 template <int D, bool BIAS>
-__device__ __forceinline__ void attend(const AttnArgs &a, Rows<D, BIAS> &r, const char *kt, const char *vt, const TileLane<D> &t, int j0, int hh) {
-    f32x16 s;
-    mfma_rows<D>(s, kt, t, r.q);
-    const float sl = BIAS ? 1.0f : a.sl2;
-    if (BIAS) add_bias<D, BIAS>(a, r, s, j0, hh);
+__device__ __forceinline__ void mask_scores(const Rows<D, BIAS> &r, f32x16 &s, int j0, int hh) {
     if (j0 + 32 > r.lim_min) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             if (j0 + acc_row(i, hh) >= r.lim) s[i] = -__builtin_inff();
     }
-    f32x16 p;
-    float sum = 0.f, mc = r.m * sl;
+}
+
+// The exponentials of a tile's scores, as the next product's operand, and their sum.  The sum is of the rounded values, two to an
+// instruction, where the log-sum-exp is not wanted: normalised by what was summed up, the outputs are a little nearer to the exact ones then.
+template <bool EXACT_SUM>
+__device__ __forceinline__ float exponentials(const f32x16 &s, float sl, float mc, BFrag (&b)[2]) {
+    float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(s[i] * sl - mc);
-        sum += p[i];
+    for (int k = 0; k < 8; ++k) {
+        const float x = __builtin_amdgcn_exp2f(s[2 * k] * sl - mc), y = __builtin_amdgcn_exp2f(s[2 * k + 1] * sl - mc);
+        const uint32_t xy = pack_bf16(x, y);
+        b[k / 4].u[k % 4] = xy;
+        if (EXACT_SUM) {
+            sum += x;
+            sum += y;
+        } else {
+            sum = add_pair(xy, sum);
+        }
     }
+    return sum;
+}
+
+// One tile of 32 keys from key j0 of the sequence on.  Where a sum exceeds the limit, the running maximum is raised, what was summed so
+// far rescaled, and the tile's exponentials done again.
+template <int D, bool BIAS, bool EXACT_SUM>
+__device__ __forceinline__ void attend(const AttnArgs &a, Rows<D, BIAS> &r, const char *kt, const char *vt, const TileLane<D> &t, int j0, int hh) {
+    f32x16 s;
+    mfma_rows<D>(s, kt, t, r.q);
+    const float sl = BIAS ? 1.0f : a.sl2;
+    if (BIAS) add_bias<D, BIAS>(a, r, s, j0, hh);
+    mask_scores<D, BIAS>(r, s, j0, hh);
+    BFrag b[2];
+    float sum = exponentials<EXACT_SUM>(s, sl, r.m * sl, b);
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kSumLimit)) != 0, 0)) {
         mfma_settle();  // the accumulators of the tile before may be in flight
         float mx = s[0];
@@ -102,21 +123,14 @@ __device__ __forceinline__ void attend(const AttnArgs &a, Rows<D, BIAS> &r, cons
         const float alpha = __builtin_amdgcn_exp2f((r.m - m_new) * sl);
         r.m = m_new;
         r.l *= alpha;
+        // (in place: as ordinary code it made the compiler copy all accumulators on the way that is nearly always taken)
 #pragma unroll
         for (int dt = 0; dt < AttnGeo<D>::ND; ++dt)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) r.o[dt][i] *= alpha;
-        mc = m_new * sl;
-        sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            p[i] = __builtin_amdgcn_exp2f(s[i] * sl - mc);
-            sum += p[i];
-        }
+            for (int i = 0; i < 16; ++i) asm volatile("v_mul_f32 %0, %1, %0" : "+v"(r.o[dt][i]) : "v"(alpha));
+        sum = exponentials<EXACT_SUM>(s, sl, m_new * sl, b);
     }
     r.l += sum;
-    BFrag b[2];
-    to_b_operand(p, b);
     mfma_transposed<D>(r.o, vt, t, b);
 }
 
@@ -125,7 +139,7 @@ constexpr int kStage = 64;  // keys per stage
 template <int D>
 constexpr int kForwardLds = 2 * kStage * 2 * AttnGeo<D>::ROW;
 
-template <int D, bool BIAS>
+template <int D, bool BIAS, bool LSE>
 __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
     using G = AttnGeo<D>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -147,27 +161,31 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
     const char *vb = reinterpret_cast<const char *>(a.v + s.k0 * a.vs[0] + head_kv * a.vs[1]);
     const uint32_t k_row = (uint32_t)a.ks[0] * 2, v_row = (uint32_t)a.vs[0] * 2;
     const CopyLane<D> c(lane);
-    auto copy_stage = [&](int st) {
-        char *at = lds + (st & 1) * (2 * kStage * G::ROW);
+    auto copy_stage = [&](int st, char *at) {
         const int j0 = st * kStage;
         copy_rows<D, kStage, 4>(kb + (uint64_t)j0 * k_row, k_row, keys - j0, at, wave, c);
         copy_rows<D, kStage, 4>(vb + (uint64_t)j0 * v_row, v_row, keys - j0, at + kStage * G::ROW, wave, c);
     };
-    if (n_st > 0) copy_stage(0);
+    if (n_st > 0) copy_stage(0, lds);
     float *tab = reinterpret_cast<float *>(lds + kForwardLds<D>);
     if (BIAS) expand_bias(a, head_kv, tab, 256);
     Rows<D, BIAS> r;
     load_rows<D, BIAS>(a, s, head_kv, v0 + wave * 32, lane, tab, r);
     const TileLane<D> t(lane);
-    for (int st = 0; st < n_st; ++st) {
+    // (two stages to a turn, so that places in LDS are constants and cost no arithmetic)
+    auto stage = [&](int st, char *at, char *next) {
         wait_copies<0>();
         wg_barrier();
-        if (st + 1 < n_st) copy_stage(st + 1);
-        const char *at = lds + (st & 1) * (2 * kStage * G::ROW);
+        if (st + 1 < n_st) copy_stage(st + 1, next);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
             if (st * kStage + 32 * h < r.lim_max)
-                attend<D, BIAS>(a, r, at + h * G::TILE, at + (kStage + 32 * h) * G::ROW, t, st * kStage + 32 * h, hh);
+                attend<D, BIAS, LSE>(a, r, at + h * G::TILE, at + (kStage + 32 * h) * G::ROW, t, st * kStage + 32 * h, hh);
+    };
+    constexpr int STAGE = 2 * kStage * G::ROW;
+    for (int st = 0; st < n_st; st += 2) {
+        stage(st, lds, lds + STAGE);
+        if (st + 1 < n_st) stage(st + 1, lds + STAGE, lds);
     }
     wait_copies<0>();
     wg_barrier();
@@ -176,7 +194,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
     const int row = v0 + wave * 32 + (lane & 31);
     const bool live = row < n_rows;
     store_query_rows<D>(a, s, head_kv, v0 + wave * 32, slot_rows, r.o, inv, live, lds + wave * 32 * G::OUT_ROW, a.out, a.os, lane);
-    if (a.lse != nullptr && hh == 0 && row < slot_rows) {
+    if (LSE && hh == 0 && row < slot_rows) {
         const int tok = (unsigned)row / (unsigned)a.group, g = row - tok * a.group;
         a.lse[(int64_t)(s.q0 + tok) * a.h_q + head_kv * a.group + g] =
             live && inv != 0.f ? (r.m * (BIAS ? 1.0f : a.sl2) + __builtin_amdgcn_logf(l)) * kLn2 : -__builtin_inff();
@@ -330,7 +348,7 @@ __global__ __launch_bounds__((64 * kFewWaves<D, SPLIT || BIAS>), 1) void attn_fe
             wait_copies<0>();
         }
         const char *at = ring + slot * 2 * G::TILE;
-        attend<D, BIAS>(a, r, at, at + G::TILE, t, j0, hh);
+        attend<D, BIAS, true>(a, r, at, at + G::TILE, t, j0, hh);
     }
     // the wavefronts' sums meet in LDS
     mfma_settle();
@@ -444,8 +462,10 @@ lsrm_status launch_forward_d(AttnArgs a, void *ws, hipStream_t st) {
     const bool bias = a.n_buckets > 0;
     if (way == MANY) {
         a.n_slots = (int)((int64_t)a.n_q * a.group / 128 + a.n_seq);
-        return launch_attn(bias ? &attn_forward_kernel<D, true> : &attn_forward_kernel<D, false>, (int64_t)a.n_slots * a.h_kv, 256,
-                           kForwardLds<D> + tab, a, st);
+        const bool lse = a.lse != nullptr;
+        auto kernel = bias ? (lse ? &attn_forward_kernel<D, true, true> : &attn_forward_kernel<D, true, false>)
+                           : (lse ? &attn_forward_kernel<D, false, true> : &attn_forward_kernel<D, false, false>);
+        return launch_attn(kernel, (int64_t)a.n_slots * a.h_kv, 256, kForwardLds<D> + tab, a, st);
     }
     const int64_t n_tiles = slots32 * a.h_kv;
     if (way == FEW)

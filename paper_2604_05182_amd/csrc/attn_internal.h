@@ -214,36 +214,29 @@ __device__ __forceinline__ void mfma_rows(f32x16 &acc, const char *tile, const T
         acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_row_frag<D>(tile, t, ks), b[ks], acc, 0, 0, 0);
 }
 
-// The transposing loads are inline assembly: the compiler cannot tell that the builtin leaves alone what copies in flight
-// are filling, and would wait for all of those first.  Their results are waited for by hand, counted (LDS operations of a
-// wavefront complete in order; others in flight only make the waits longer).
-template <int OFF>
-__device__ __forceinline__ void tr_issue(BFrag &f, uint32_t a0, uint32_t a1) {
-    asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%4\n\tds_read_b64_tr_b16 %1, %3 offset:%4"
-                 : "=&v"(f.h[0]), "=&v"(f.h[1])
-                 : "v"(a0), "v"(a1), "n"(OFF)
-                 : "memory");
+// fragment (ks2, dt) of the transposed tile.  (The copies to LDS are inline assembly, so the compiler knows of none that this load would
+// have to wait for.)
+template <int D>
+__device__ __forceinline__ bf16x8 read_tr_frag(const char *tile, const TileLane<D> &t, int ks2, int dt) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const int at = dt / 2 * 128 + ks2 * 16 * AttnGeo<D>::ROW;
+    union {
+        s16x4 h[2];
+        bf16x8 v;
+    } u;
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + t.tr[0][dt % 2] + at));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + t.tr[1][dt % 2] + at));
+    return u.v;
 }
-template <int N>
-__device__ __forceinline__ bf16x8 tr_take(BFrag &f) {
-    asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(f.h[0]), "+v"(f.h[1]) : "n"(N) : "memory");
-    return f.v;
-}
-// acc[dt] += (transposed tile: channels x 32 rows) x b[ks2] for every dt and ks2; all fragments requested at once, each MFMA waits for its own
-template <int D, int... I>
-__device__ __forceinline__ void mfma_transposed_impl(f32x16 (&acc)[AttnGeo<D>::ND], const uint32_t (&a0)[2], const uint32_t (&a1)[2],
-                                                     const BFrag (&b)[2], std::integer_sequence<int, I...>) {
-    constexpr int ND = AttnGeo<D>::ND;
-    BFrag f[2 * ND];
-    (tr_issue<(I % ND) / 2 * 128 + (I / ND) * 16 * AttnGeo<D>::ROW>(f[I], a0[(I % ND) % 2], a1[(I % ND) % 2]), ...);
-    ((acc[I % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_take<2 * (2 * ND - 1 - I)>(f[I]), b[I / ND].v, acc[I % ND], 0, 0, 0)), ...);
-}
+// acc[dt] += (transposed tile: channels x 32 rows) x b[ks2] for every dt and ks2
 template <int D>
 __device__ __forceinline__ void mfma_transposed(f32x16 (&acc)[AttnGeo<D>::ND], const char *tile, const TileLane<D> &t, const BFrag (&b)[2]) {
-    const uint32_t at = (uint32_t)(uintptr_t)tile;  // (the low 32 bits of a generic pointer into LDS are the LDS address)
-    constexpr int P1 = AttnGeo<D>::ND < 2 ? 0 : 1;
-    const uint32_t a0[2] = {at + t.tr[0][0], at + t.tr[0][P1]}, a1[2] = {at + t.tr[1][0], at + t.tr[1][P1]};
-    mfma_transposed_impl<D>(acc, a0, a1, b, std::make_integer_sequence<int, 2 * AttnGeo<D>::ND>{});
+#pragma unroll
+    for (int ks2 = 0; ks2 < 2; ++ks2)
+#pragma unroll
+        for (int dt = 0; dt < AttnGeo<D>::ND; ++dt)
+            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr_frag<D>(tile, t, ks2, dt), b[ks2].v, acc[dt], 0, 0, 0);
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
@@ -251,6 +244,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     p[0] = (__bf16)a;
     p[1] = (__bf16)b;
     return *reinterpret_cast<uint32_t *>(&p);
+}
+// sum + both values of a pair
+__device__ __forceinline__ float add_pair(uint32_t xy, float sum) {
+    const uint32_t ones = 0x3f803f80u;
+    return __builtin_amdgcn_fdot2_f32_bf16(*reinterpret_cast<const bf16x2 *>(&xy), *reinterpret_cast<const bf16x2 *>(&ones), sum, false);
 }
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
