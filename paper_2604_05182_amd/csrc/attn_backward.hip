@@ -33,12 +33,12 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv, place = blockIdx.x / a.h_kv;
     const int part = place % a.parts;
-    const int slot = a.causal ? a.n_slots - 1 - place / a.parts : place / a.parts;
-    int tile;
-    const Sequence s = find_tile<false>(a, a.group, 128, slot, &tile);
-    const int v_wg = tile * 128, slot_rows = s.q_slot * a.group;
-    const int n_rows = s.n_q * a.group;
-    if (v_wg < 0 || v_wg >= slot_rows) return;
+    int tile, seq;
+    Sequence s;
+    if (!find_tile<false>(a, a.group, 128, place / a.parts, s, tile, seq)) return;
+    const int slot_rows = s.q_slot * a.group, n_rows = s.n_q * a.group;
+    if (a.causal) tile = (slot_rows - 1) / 128 - tile;  // the last rows, which see most keys, first
+    const int v_wg = tile * 128;
     auto seen = [&](int pos) { return a.causal ? min(max(pos + 1, 0), s.n_k) : s.n_k; };
     const int keys = v_wg < n_rows ? seen(uniform((unsigned)min(v_wg + 127, n_rows - 1) / (unsigned)a.group) + s.shift) : 0;
     const int st_all = (keys + kStage - 1) / kStage, st_per = uniform((st_all + a.parts - 1) / a.parts);
@@ -89,6 +89,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     for (int dt = 0; dt < G::ND; ++dt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) dq[dt][i] = 0.f;
+    const f32x16 minus_delta = splat(-delta);  // (what dP is added to: no instruction of its own takes D off)
     float miss = 0.f;  // sum of dS over this lane's keys
     const float *tab_g = tab + g * a.tab;
     const TileLane<D> t(lane);
@@ -102,9 +103,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
             const int j0 = st * kStage + 32 * h;
             if (j0 >= lim_max) continue;
             const char *kt = at + h * G::TILE, *vt = at + (kStage + 32 * h) * G::ROW;
-            f32x16 x, dp;
-            mfma_rows<D>(x, kt, t, q);
-            mfma_rows<D>(dp, vt, t, dout);
+            f32x16 x = mfma_rows<D>(splat(0.f), kt, t, q), dp = mfma_rows<D>(minus_delta, vt, t, dout);
             const bool behind = BIAS && j0 + 31 - pos_min < a.b0, ahead = BIAS && j0 - pos_max >= a.b_last;
             if (BIAS) {
                 if (behind || ahead) {
@@ -124,7 +123,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                dp[i] = __builtin_amdgcn_exp2f(BIAS ? x[i] - off : x[i] * a.sl2 - off) * (dp[i] - delta);
+                dp[i] = __builtin_amdgcn_exp2f(BIAS ? x[i] - off : x[i] * a.sl2 - off) * dp[i];
                 miss += dp[i];
             }
             BFrag b[2];
@@ -239,11 +238,11 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv, place = blockIdx.x / a.h_kv;
-    const int part = place % a.parts, slot = place / a.parts;
-    int tile;
-    const Sequence s = find_tile<true>(a, 1, 128, slot, &tile);
+    const int part = place % a.parts;
+    int tile = 0, seq;
+    Sequence s = {};
+    const bool none = !find_tile<true>(a, 1, 128, place / a.parts, s, tile, seq);
     const int j_wg = tile * 128;
-    const bool none = j_wg < 0 || j_wg >= s.k_slot;
     const int j0 = j_wg + wave * 32, j = j0 + (lane & 31);
     const bool live = j < s.n_k;
     // query tiles of 32: those of a head from the first that sees a key of this workgroup on, head after head
@@ -332,8 +331,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
             if (j0 < s.n_k && !(a.causal && p0 + 31 < j0)) {
                 const char *at = lds + ((i - i_begin) & (RING - 1)) * kDkvSlot<D>;
                 const float *aux = reinterpret_cast<const float *>(at + 2 * G::TILE) + 8 * hh;
-                f32x16 p, dp;
-                mfma_rows<D>(p, at, t, kf);
+                f32x16 p = mfma_rows<D>(splat(0.f), at, t, kf), dp;
                 const bool behind = BIAS && j0 + 31 - p0 < a.b0, ahead = BIAS && j0 - p0 - 31 >= a.b_last;
                 if (BIAS) {
                     const float *tab_g = tab + g * a.tab;
@@ -365,22 +363,23 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
                 BFrag b[2];
                 to_b_operand(p, b);
                 mfma_transposed<D>(dv, at + G::TILE, t, b);
-                if constexpr (V_LDS) {
+                // dP - D: the product is added to -D
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) dp[e] = 0.f;
+                for (int e4 = 0; e4 < 16; e4 += 4) {
+                    const f32x4 nd = *reinterpret_cast<const f32x4 *>(aux + 32 + 16 * (e4 / 8) + e4 % 8);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dp[e4 + e] = nd[e];
+                }
+                if constexpr (V_LDS) {
 #pragma unroll
                     for (int ks = 0; ks < G::NS; ++ks)
                         dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_row_frag<D>(at + G::TILE, t, ks),
                                                                      *reinterpret_cast<const bf16x8 *>(values + ks * 1024), dp, 0, 0, 0);
                 } else {
-                    mfma_rows<D>(dp, at + G::TILE, t, vf);
+                    dp = mfma_rows<D>(dp, at + G::TILE, t, vf);
                 }
 #pragma unroll
-                for (int e4 = 0; e4 < 16; e4 += 4) {
-                    const f32x4 nd = *reinterpret_cast<const f32x4 *>(aux + 32 + 16 * (e4 / 8) + e4 % 8);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) dp[e4 + e] = p[e4 + e] * (dp[e4 + e] + nd[e]);
-                }
+                for (int e = 0; e < 16; ++e) dp[e] *= p[e];
                 if (BIAS && sums != nullptr) {
                     if (behind || ahead) {
                         float sum = 0.f;
@@ -453,10 +452,10 @@ template <int D, bool Q>
 __global__ __launch_bounds__(256) void attn_sum_parts(AttnArgs a) {
     const int heads = Q ? a.h_q : a.h_kv, n = Q ? a.n_q : a.n_k;
     const int head = blockIdx.x % heads, slot = blockIdx.x / heads;
-    int tile;
-    const Sequence s = find_tile<!Q>(a, 1, 128, slot, &tile);
+    int tile, seq;
+    Sequence s;
+    if (!find_tile<!Q>(a, 1, 128, slot, s, tile, seq)) return;
     const int first = tile * 128, rows = Q ? s.q_slot : s.k_slot, row0 = Q ? s.q0 : s.k0;
-    if (first < 0 || first >= rows) return;
     constexpr int CH = D / 8;
     const int64_t step = (int64_t)n * heads * D;
     if (Q && threadIdx.x < 128 && first + (int)threadIdx.x < s.n_q) {

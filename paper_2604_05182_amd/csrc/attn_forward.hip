@@ -107,8 +107,7 @@ __device__ __forceinline__ float exponentials(const f32x16 &s, float sl, float m
 // far rescaled, and the tile's exponentials done again.
 template <int D, bool BIAS, bool EXACT_SUM>
 __device__ __forceinline__ void attend(const AttnArgs &a, Rows<D, BIAS> &r, const char *kt, const char *vt, const TileLane<D> &t, int j0, int hh) {
-    f32x16 s;
-    mfma_rows<D>(s, kt, t, r.q);
+    f32x16 s = mfma_rows<D>(splat(0.f), kt, t, r.q);
     const float sl = BIAS ? 1.0f : a.sl2;
     if (BIAS) add_bias<D, BIAS>(a, r, s, j0, hh);
     mask_scores<D, BIAS>(r, s, j0, hh);
@@ -145,11 +144,12 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv;
-    const int slot = a.causal ? a.n_slots - 1 - (int)(blockIdx.x / a.h_kv) : (int)(blockIdx.x / a.h_kv);
-    int tile;
-    const Sequence s = find_tile<false>(a, a.group, 128, slot, &tile);
-    const int v0 = tile * 128, slot_rows = s.q_slot * a.group;
-    if (v0 < 0 || v0 >= slot_rows) return;
+    int tile, seq;
+    Sequence s;
+    if (!find_tile<false>(a, a.group, 128, blockIdx.x / a.h_kv, s, tile, seq)) return;
+    const int slot_rows = s.q_slot * a.group;
+    if (a.causal) tile = (slot_rows - 1) / 128 - tile;  // the last rows, which see most keys, first
+    const int v0 = tile * 128;
     const int n_rows = s.n_q * a.group;
     int keys = 0;  // that the last live row sees, hence any
     if (v0 < n_rows) {
@@ -301,15 +301,15 @@ __global__ __launch_bounds__((64 * kFewWaves<D, SPLIT || BIAS>), 1) void attn_fe
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv, unit = blockIdx.x / a.h_kv;
-    int tile, part = 0, n_parts = 1, chunk = 0;
+    int tile, seq, part = 0, n_parts = 1, chunk = 0;
     Sequence s;
     if (SPLIT) {
         chunk = part_keys(a);
-        const int seq = uniform(unit_sequence(a, unit, chunk, &tile));
+        seq = uniform(unit_sequence(a, unit, chunk, &tile));
         if (seq >= a.n_seq) return;
         s = load_sequence(a, seq);
-    } else {
-        s = find_tile<false>(a, a.group, kFewRows, unit, &tile);
+    } else if (!find_tile<false>(a, a.group, kFewRows, unit, s, tile, seq)) {
+        return;
     }
     if (SPLIT) {
         n_parts = uniform(parts_of(s, chunk));
@@ -405,9 +405,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
     __shared__ float part_max[4], part_sum[4];
     const int way = blockIdx.x % kJoinWays, head_kv = blockIdx.x / kJoinWays % a.h_kv, slot = blockIdx.x / kJoinWays / a.h_kv;
     int tile, seq;
-    const Sequence s = find_tile<false>(a, a.group, kFewRows, slot, &tile, &seq);
+    Sequence s;
+    if (!find_tile<false>(a, a.group, kFewRows, slot, s, tile, seq)) return;
     const int slot_rows = s.q_slot * a.group;
-    if (tile < 0 || tile * kFewRows + way >= slot_rows) return;
+    if (tile * kFewRows + way >= slot_rows) return;
     const int chunk = part_keys(a), n_parts = parts_of(s, chunk);
     if (n_parts == 1) return;
     const int unit = units_before(a, seq, chunk) + tile * n_parts;

@@ -27,7 +27,7 @@ struct AttnArgs {
     const int32_t *q_off, *k_off, *q_len, *k_len;
     int64_t qs[2], ks[2], vs[2], os[2];  // {row, head} strides in elements
     int n_q, n_k, n_seq, h_q, h_kv, group, causal;
-    int n_slots;           // row tiles of all sequences at most (see find_tile)
+    int n_slots;           // tiles of query rows of all sequences at most (see find_tile)
     int unit_cap;          // forward of few rows: units of all sequences at most
     int parts;             // backward: parts that a walk is cut into
     float *part;           // forward of few rows: sums of the parts
@@ -60,7 +60,9 @@ struct Sequence {
     int shift;  // position of query 0
 };
 // (whatever the offsets and lengths hold, the rows lie in the tensors)
-__device__ __forceinline__ Sequence sequence_of(const AttnArgs &a, int q0, int q1, int k0, int k1, int q_len, int k_len) {
+__device__ __forceinline__ Sequence load_sequence(const AttnArgs &a, int s) {
+    const int q0 = a.q_off[s], q1 = a.q_off[s + 1], k0 = a.k_off[s], k1 = a.k_off[s + 1];
+    const int q_len = a.q_len != nullptr ? a.q_len[s] : 0, k_len = a.k_len != nullptr ? a.k_len[s] : 0;
     Sequence r;
     r.q0 = min(max(q0, 0), a.n_q);
     r.q_slot = min(max(q1, r.q0), a.n_q) - r.q0;
@@ -71,50 +73,56 @@ __device__ __forceinline__ Sequence sequence_of(const AttnArgs &a, int q0, int q
     r.shift = r.n_k - r.n_q;
     return r;
 }
-__device__ __forceinline__ Sequence load_sequence(const AttnArgs &a, int s) {
-    return sequence_of(a, a.q_off[s], a.q_off[s + 1], a.k_off[s], a.k_off[s + 1], a.q_len != nullptr ? a.q_len[s] : 0,
-                       a.k_len != nullptr ? a.k_len[s] : 0);
-}
 
-// Tiles of `bm` rows have slots of their own without anyone counting them: sequence s starts at slot floor(first row / bm) + s, and has
-// at most as many tiles as there are slots up to the next one's start.  find_tile returns the last sequence that starts at or before
-// slot x, and the number of the tile there (which may be none of its tiles): a wavefront probes 64 places at a time.  Up to 64 sequences each lane
-// loads one of them whole, so that there is one trip to memory, not two (0.7 us of every small kernel); two rounds of probes up to 4096.
+// Which tile of `bm` rows (of the keys: KEYS, else of the queries) is x?  Up to 64 sequences, a lane of the wavefront loads each and counts its
+// tiles; those of the sequences that take longest come first, so that what runs last is short.  False if there are fewer tiles.
+// Beyond, sequence s has the tiles from number floor(first row / bm) + s on -- room for all of its own, and nobody needs to count -- and is
+// found by probing 64 places at a time; then some numbers are no tile.
 __device__ __forceinline__ int tile_slot(int off, int n_rows, int mult, int bm, int s) { return min(max(off, 0), n_rows) * mult / bm + s; }
 template <bool KEYS>
-__device__ __forceinline__ Sequence find_tile(const AttnArgs &a, int mult, int bm, int x, int *tile, int *seq = nullptr) {
+__device__ __forceinline__ bool find_tile(const AttnArgs &a, int mult, int bm, int x, Sequence &s, int &tile, int &seq) {
     const int lane = threadIdx.x & 63, n_rows = KEYS ? a.n_k : a.n_q;
-    const int32_t *off = KEYS ? a.k_off : a.q_off;
     if (a.n_seq <= 64) {
-        const int i = min(lane, a.n_seq - 1);
-        const int q0 = a.q_off[i], q1 = a.q_off[i + 1], k0 = a.k_off[i], k1 = a.k_off[i + 1];
-        const int q_len = a.q_len != nullptr ? a.q_len[i] : 0, k_len = a.k_len != nullptr ? a.k_len[i] : 0;
-        const int start = tile_slot(KEYS ? k0 : q0, n_rows, mult, bm, i);
-        const uint64_t after = ~__builtin_amdgcn_ballot_w64(lane < a.n_seq && start <= x);
-        const int at = max(after == 0 ? 63 : (int)__builtin_ctzll(after) - 1, 0);
-        *tile = x - __builtin_amdgcn_readlane(start, at);
-        if (seq != nullptr) *seq = at;
-        return sequence_of(a, __builtin_amdgcn_readlane(q0, at), __builtin_amdgcn_readlane(q1, at), __builtin_amdgcn_readlane(k0, at),
-                           __builtin_amdgcn_readlane(k1, at), __builtin_amdgcn_readlane(q_len, at), __builtin_amdgcn_readlane(k_len, at));
+        const Sequence mine = load_sequence(a, min(lane, a.n_seq - 1));
+        const int rows = (KEYS ? mine.k_slot : mine.q_slot) * mult, tiles = lane < a.n_seq ? (rows + bm - 1) / bm : 0;
+        const int work = KEYS ? mine.n_q : mine.n_k;
+        int first = 0;
+        for (int i = 0; i < a.n_seq; ++i) {
+            const int w = __builtin_amdgcn_readlane(work, i), n = __builtin_amdgcn_readlane(tiles, i);
+            first += w > work || (w == work && i < lane) ? n : 0;
+        }
+        const uint64_t found = __builtin_amdgcn_ballot_w64(first <= x && x < first + tiles);
+        if (found == 0) return false;
+        seq = __builtin_ctzll(found);
+        tile = x - __builtin_amdgcn_readlane(first, seq);
+        s.q0 = __builtin_amdgcn_readlane(mine.q0, seq);
+        s.n_q = __builtin_amdgcn_readlane(mine.n_q, seq);
+        s.q_slot = __builtin_amdgcn_readlane(mine.q_slot, seq);
+        s.k0 = __builtin_amdgcn_readlane(mine.k0, seq);
+        s.n_k = __builtin_amdgcn_readlane(mine.n_k, seq);
+        s.k_slot = __builtin_amdgcn_readlane(mine.k_slot, seq);
+        s.shift = s.n_k - s.n_q;
+        return true;
     }
+    const int32_t *off = KEYS ? a.k_off : a.q_off;
     int lo = 0, hi = a.n_seq;
     while (hi - lo > 1) {
-        const int step = (hi - lo + 63) / 64, s = lo + (lane + 1) * step;
-        const uint64_t below = __builtin_amdgcn_ballot_w64(s < hi && tile_slot(off[min(s, a.n_seq - 1)], n_rows, mult, bm, s) <= x);
+        const int step = (hi - lo + 63) / 64, i = lo + (lane + 1) * step;
+        const uint64_t below = __builtin_amdgcn_ballot_w64(i < hi && tile_slot(off[min(i, a.n_seq - 1)], n_rows, mult, bm, i) <= x);
         const int c = __builtin_ctzll(~below);  // (the last lane's place is never below hi)
         lo += c * step;
         hi = min(hi, lo + step);
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    *tile = x - tile_slot(off[lo], n_rows, mult, bm, lo);
-    if (seq != nullptr) *seq = lo;
-    return load_sequence(a, lo);
+    seq = uniform(lo);
+    tile = x - tile_slot(off[seq], n_rows, mult, bm, seq);
+    s = load_sequence(a, seq);
+    return tile >= 0 && (int64_t)tile * bm < (int64_t)(KEYS ? s.k_slot : s.q_slot) * mult;
 }
 
 // ---- tiles in LDS ----------------------------------------------------------------------------------------------------
 // A tile is 32 rows of one head, row-major, as they are in memory; the 16-byte chunks of a row change places by a key of its row
-// number, so that reads of one chunk of many rows (MFMA operands along the channels) and of few chunks of four rows
-// (transposing reads) both spread over all banks.
+// number, so that reads of one chunk of 16 rows (MFMA operands along the channels) and of four chunks of four rows
+// (transposing reads), what the 64 banks serve at a time, have no bank twice.
 template <int D>
 struct AttnGeo {
     static constexpr int NS = D / 16, ND = D / 32;  // 16-channel slabs, 32-channel tiles
@@ -122,13 +130,12 @@ struct AttnGeo {
     static constexpr int TILE = 32 * ROW;
     static constexpr int RPC = 1024 / ROW;          // rows per copy instruction
     static constexpr int COPIES = TILE / 1024;      // copy instructions per tile
-    static constexpr int NX = NS < 4 ? NS : 4;      // addresses for reads along the channels
     static constexpr int OUT_ROW = 2 * D + 16;      // padded row of the output staging (bytes)
 };
 template <int D>
 __device__ __forceinline__ int row_key(int r) {
-    const int b = ((r >> 2) ^ (r >> 3)) & 1;
-    return D == 32 ? (((r >> 1) & 1) << 1) | b : ((r & 3) << 1) | b;
+    const int low = (r >> 2) & 3;
+    return D == 128 ? ((r & 3) << 2) | low : D == 64 ? (((r >> 1) & 1) << 2) | low : low;
 }
 // row permutation of the operand whose product becomes the next contraction's operand: bits 2 and 3 swapped
 __device__ __forceinline__ int perm32(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
@@ -136,7 +143,7 @@ __device__ __forceinline__ int perm32(int r) { return (r & ~12) | ((r & 4) << 1)
 // Where this lane's 16 bytes of copy instruction i of a tile come from: row of the tile, byte in the row
 template <int D>
 struct CopyLane {
-    int row, chunk;  // of instruction 0; the others add i * RPC rows and xor the chunk's lowest bit (copy_flip)
+    int row, chunk;  // of instruction 0; the others add i * RPC rows and change two bits of the chunk (copy_flip)
     __device__ explicit CopyLane(int lane) {
         row = lane * 16 / AttnGeo<D>::ROW;
         chunk = (lane * 16 % AttnGeo<D>::ROW) / 16 ^ row_key<D>(row);
@@ -144,7 +151,7 @@ struct CopyLane {
 };
 template <int D>
 __device__ __forceinline__ constexpr int copy_flip(int i) {
-    return D == 128 ? (i ^ (i >> 1)) & 1 : D == 64 ? i & 1 : 0;
+    return D == 128 ? i & 3 : D == 64 ? (i & 1) << 1 : 0;
 }
 
 // Copies the instructions first, first + step, ... of n rows (a multiple of 32, tiles behind each other) from src, rows stride_b bytes apart, to
@@ -170,25 +177,25 @@ __device__ __forceinline__ void copy_rows(const char *src, uint32_t stride_b, in
 }
 
 // Addresses of MFMA A operands in a tile (add the tile's own):
-//   rows   fragment ks: lane (hh = lane / 32, r): row perm32(r), channels 16 ks + 8 hh + 0..7     at at[ks % 4] + 128 (ks / 4)
+//   rows   fragment ks: lane (hh = lane / 32, r): row perm32(r), channels 16 ks + 8 hh + 0..7     at at[ks]
 //   transp fragment (ks2, dt): lane (hh, r): channel 32 dt + r, rows 16 ks2 + 8 hh + 0..7: two transposing loads of four rows
 //          (ds_read_b64_tr_b16: in each group of 16 lanes, lane j gets as element e the 16-bit element j % 4 of what lane
-//          4 e + j / 4 addressed), at tr[half][dt % 2] + 128 (dt / 2) + 16 ks2 rows
+//          4 e + j / 4 addressed), at tr[half][dt] + 16 ks2 rows
 template <int D>
 struct TileLane {
-    uint32_t at[AttnGeo<D>::NX], tr[2][AttnGeo<D>::ND < 2 ? 1 : 2];
+    uint32_t at[AttnGeo<D>::NS], tr[2][AttnGeo<D>::ND];
     __device__ explicit TileLane(int lane) {
         using G = AttnGeo<D>;
         const int hh = lane >> 5, r = perm32(lane & 31);
 #pragma unroll
-        for (int x = 0; x < G::NX; ++x) at[x] = r * G::ROW + (((2 * x + hh) ^ row_key<D>(r)) << 4);
+        for (int x = 0; x < G::NS; ++x) at[x] = r * G::ROW + (((2 * x + hh) ^ row_key<D>(r)) << 4);
         const int s = lane & 15, half16 = (lane >> 4) & 1;
 #pragma unroll
         for (int h2 = 0; h2 < 2; ++h2)
 #pragma unroll
-            for (int p = 0; p < (G::ND < 2 ? 1 : 2); ++p) {
+            for (int dt = 0; dt < G::ND; ++dt) {
                 const int row = 8 * hh + 4 * h2 + (s >> 2);
-                tr[h2][p] = row * G::ROW + (((4 * p + 2 * half16 + ((s & 3) >> 1)) ^ row_key<D>(row)) << 4) + ((s & 1) << 3);
+                tr[h2][dt] = row * G::ROW + (((4 * dt + 2 * half16 + ((s & 3) >> 1)) ^ row_key<D>(row)) << 4) + ((s & 1) << 3);
             }
     }
 };
@@ -201,17 +208,23 @@ union BFrag {
 
 template <int D>
 __device__ __forceinline__ bf16x8 read_row_frag(const char *tile, const TileLane<D> &t, int ks) {
-    return *reinterpret_cast<const bf16x8 *>(tile + t.at[ks % AttnGeo<D>::NX] + (ks / 4) * 128);
+    return *reinterpret_cast<const bf16x8 *>(tile + t.at[ks]);
 }
 
-// acc = (rows of the tile) x b over all channels
+// start + (rows of the tile) x b over all channels
 template <int D>
-__device__ __forceinline__ void mfma_rows(f32x16 &acc, const char *tile, const TileLane<D> &t, const bf16x8 (&b)[AttnGeo<D>::NS]) {
+__device__ __forceinline__ f32x16 mfma_rows(const f32x16 &start, const char *tile, const TileLane<D> &t, const bf16x8 (&b)[AttnGeo<D>::NS]) {
+    f32x16 acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_row_frag<D>(tile, t, 0), b[0], start, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < AttnGeo<D>::NS; ++ks)
+    for (int ks = 1; ks < AttnGeo<D>::NS; ++ks)
         acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_row_frag<D>(tile, t, ks), b[ks], acc, 0, 0, 0);
+    return acc;
+}
+__device__ __forceinline__ f32x16 splat(float x) {
+    f32x16 r;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = x;
+    return r;
 }
 
 // fragment (ks2, dt) of the transposed tile.  (The copies to LDS are inline assembly, so the compiler knows of none that this load would
@@ -220,13 +233,13 @@ template <int D>
 __device__ __forceinline__ bf16x8 read_tr_frag(const char *tile, const TileLane<D> &t, int ks2, int dt) {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const int at = dt / 2 * 128 + ks2 * 16 * AttnGeo<D>::ROW;
+    const int at = ks2 * 16 * AttnGeo<D>::ROW;
     union {
         s16x4 h[2];
         bf16x8 v;
     } u;
-    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + t.tr[0][dt % 2] + at));
-    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + t.tr[1][dt % 2] + at));
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + t.tr[0][dt] + at));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + t.tr[1][dt] + at));
     return u.v;
 }
 // acc[dt] += (transposed tile: channels x 32 rows) x b[ks2] for every dt and ks2
