@@ -500,7 +500,24 @@ __global__ __launch_bounds__(1024) void attn_sum_bias(AttnArgs a) {
     }
 }
 
-// Where there are few workgroups, walks are cut into parts, of which fp32 sums are added up afterwards.
+// Where there are few workgroups, walks are cut into parts, of which fp32 sums are added up afterwards.  How many is a trade between walks
+// that leave the chip empty and sums that are written and read; by what both take (one walk step of a workgroup: `cycles` of a chip
+// that is full from `full` workgroups on; 3.5 bytes of sums a nanosecond, and 4 us for the launch):
+//   T(parts) = steps / min(1, workgroups parts / full) + (parts > 1) (4 us + parts bytes / 3.5 TB/s)
+// Always 512 workgroups instead: 32 heads of 32 on 2, 6372 tokens 450 -> 390 us a training step.
+int best_parts(double steps, double cycles, double workgroups, double full, double bytes, int64_t walk) {
+    const double work = steps * cycles / 4 / 256 / 2.1e3;  // us, with the chip full
+    int best = 1;
+    double least = 0;
+    for (int p = 1; p <= 16 && (p == 1 || p * 4 <= walk); ++p) {
+        const double t = work / std::min(1.0, workgroups * p / full) + (p > 1 ? 4 + p * bytes / 3.5e6 : 0);
+        if (p == 1 || t < least) {
+            best = p;
+            least = t;
+        }
+    }
+    return best;
+}
 struct WsLayout {
     int q_slots, k_slots, q_parts, k_parts;
     size_t aux, part_q, part_k, part_v, part_bias, total;
@@ -510,11 +527,13 @@ WsLayout layout(const AttnArgs &a, int d) {
     const int64_t rows = (int64_t)a.n_q * a.group;
     w.q_slots = (int)(rows / 128 + a.n_seq);
     w.k_slots = a.n_k / 128 + a.n_seq;
-    auto parts = [&](int64_t wgs, int64_t walk) {  // walk: tiles of 32 that an average workgroup walks
-        return (int)std::min<int64_t>(std::max<int64_t>(512 / std::max<int64_t>(wgs, 1), 1), std::min<int64_t>(std::max<int64_t>(walk / 8, 1), 16));
-    };
-    w.q_parts = parts((rows / 128 + 1) * a.h_kv, (int64_t)a.n_k / a.n_seq / 32);
-    w.k_parts = parts(((int64_t)a.n_k / 128 + 1) * a.h_kv, rows / a.n_seq / 32);
+    // walk steps of single wavefronts (32 x 32): those of an average sequence, half of them where causal
+    const double steps = (double)rows * a.h_kv / 32 * a.n_k / a.n_seq / 32 * (a.causal && a.n_q == a.n_k ? 0.5 : 1.0);
+    const int full = d == 32 ? 1024 : 512;
+    w.q_parts = best_parts(steps, d == 32 ? 450 : d == 64 ? 600 : 1050, ((double)rows / 128 + 1) * a.h_kv, full, (double)a.n_q * a.h_q * d * 8,
+                           (int64_t)a.n_k / a.n_seq / 32);
+    w.k_parts = best_parts(steps, d == 32 ? 600 : d == 64 ? 800 : 1400, ((double)a.n_k / 128 + 1) * a.h_kv, full, (double)a.n_k * a.h_kv * d * 16,
+                           rows / a.n_seq / 32);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
