@@ -103,8 +103,8 @@ lsrm_status make_attn_args(const lsrm_attn_params *p, AttnArgs *a) {
     const int64_t most = (int64_t)1 << 30;
     if (p->n_q > most || p->n_k > most || p->n_q * (p->h_q / p->h_kv) > most) return LSRM_ERR_UNSUPPORTED;
     a->group = p->h_q / p->h_kv;
-    // workgroups of 256 threads that a launch can have
-    const int64_t wgs = (int64_t)1 << 23, rows = p->n_q * a->group;
+    // workgroups of up to 512 threads that a launch can have, two for some of these
+    const int64_t wgs = (int64_t)1 << 22, rows = p->n_q * a->group;
     if ((rows / 32 + p->n_seq) * p->h_kv > wgs || (p->n_q / 128 + p->n_seq) * p->h_q > wgs || (p->n_k / 128 + p->n_seq) * p->h_kv > wgs)
         return LSRM_ERR_UNSUPPORTED;
     if (!strides_of(p->q_stride, p->h_q, p->d, a->qs) || !strides_of(p->k_stride, p->h_kv, p->d, a->ks) ||

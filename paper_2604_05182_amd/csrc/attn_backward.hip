@@ -447,40 +447,35 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
     }
 }
 
-// Parts of dQ (Q) or of dK and dV, added in order.  A workgroup: up to 128 rows of a sequence's slot, one head.
+// Parts of dQ (Q) or of dK and dV, added in order.  A workgroup: up to 2048 / d rows of a sequence's slot, one head; eight channels to a thread.
 template <int D, bool Q>
 __global__ __launch_bounds__(256) void attn_sum_parts(AttnArgs a) {
+    constexpr int CH = D / 8, ROWS = 256 / CH;
     const int heads = Q ? a.h_q : a.h_kv, n = Q ? a.n_q : a.n_k;
-    const int head = blockIdx.x % heads, slot = blockIdx.x / heads;
+    const int which = Q ? 0 : blockIdx.x % 2, place = Q ? blockIdx.x : blockIdx.x / 2, head = place % heads;
     int tile, seq;
     Sequence s;
-    if (!find_tile<!Q>(a, 1, 128, slot, s, tile, seq)) return;
-    const int first = tile * 128, rows = Q ? s.q_slot : s.k_slot, row0 = Q ? s.q0 : s.k0;
-    constexpr int CH = D / 8;
-    const int64_t step = (int64_t)n * heads * D;
-    if (Q && threadIdx.x < 128 && first + (int)threadIdx.x < s.n_q) {
-        float2 *at = a.aux + (int64_t)head * n + row0 + first + threadIdx.x;
+    if (!find_tile<!Q>(a, 1, ROWS, place / heads, s, tile, seq)) return;
+    const int r = tile * ROWS + threadIdx.x / CH, ch = threadIdx.x % CH, row0 = Q ? s.q0 : s.k0;
+    if (r >= (Q ? s.q_slot : s.k_slot)) return;
+    if (Q && ch == 0 && r < s.n_q) {
+        float2 *at = a.aux + (int64_t)head * n + row0 + r;
         float2 x = at[0];
         for (int p = 1; p < a.parts; ++p) x.y += at[(int64_t)p * heads * n].y;
         at[0] = x;
     }
-    for (int which = 0; which < (Q ? 1 : 2); ++which) {
-        const float *from = Q ? a.part_q : which == 0 ? a.part_k : a.part_v;
-        uint16_t *dst = Q ? a.dq : which == 0 ? a.dk : a.dv;
-        const int64_t *stride = Q ? a.qs : which == 0 ? a.ks : a.vs;
-        for (int i = threadIdx.x; i < 128 * CH; i += 256) {
-            const int r = first + i / CH, ch = i % CH;
-            if (r >= rows) break;
-            const float *at = from + ((int64_t)(row0 + r) * heads + head) * D + 8 * ch;
-            f32x4 x = *reinterpret_cast<const f32x4 *>(at), y = *reinterpret_cast<const f32x4 *>(at + 4);
-            for (int p = 1; p < a.parts; ++p) {
-                x += *reinterpret_cast<const f32x4 *>(at + p * step);
-                y += *reinterpret_cast<const f32x4 *>(at + p * step + 4);
-            }
-            *reinterpret_cast<uint4 *>(dst + (int64_t)(row0 + r) * stride[0] + head * stride[1] + 8 * ch) =
-                make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-        }
+    const int64_t step = (int64_t)n * heads * D;
+    const float *at = (Q ? a.part_q : which == 0 ? a.part_k : a.part_v) + ((int64_t)(row0 + r) * heads + head) * D + 8 * ch;
+    f32x4 x = *reinterpret_cast<const f32x4 *>(at), y = *reinterpret_cast<const f32x4 *>(at + 4);
+#pragma unroll 4
+    for (int p = 1; p < a.parts; ++p) {
+        x += *reinterpret_cast<const f32x4 *>(at + p * step);
+        y += *reinterpret_cast<const f32x4 *>(at + p * step + 4);
     }
+    uint16_t *dst = Q ? a.dq : which == 0 ? a.dk : a.dv;
+    const int64_t *stride = Q ? a.qs : which == 0 ? a.ks : a.vs;
+    *reinterpret_cast<uint4 *>(dst + (int64_t)(row0 + r) * stride[0] + head * stride[1] + 8 * ch) =
+        make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
 }
 
 // The bias' gradient: what the workgroups of a head left, added in order (in 64 bits).
@@ -500,24 +495,6 @@ __global__ __launch_bounds__(1024) void attn_sum_bias(AttnArgs a) {
     }
 }
 
-// Where there are few workgroups, walks are cut into parts, of which fp32 sums are added up afterwards.  How many is a trade between walks
-// that leave the chip empty and sums that are written and read; by what both take (one walk step of a workgroup: `cycles` of a chip
-// that is full from `full` workgroups on; 3.5 bytes of sums a nanosecond, and 4 us for the launch):
-//   T(parts) = steps / min(1, workgroups parts / full) + (parts > 1) (4 us + parts bytes / 3.5 TB/s)
-// Always 512 workgroups instead: 32 heads of 32 on 2, 6372 tokens 450 -> 390 us a training step.
-int best_parts(double steps, double cycles, double workgroups, double full, double bytes, int64_t walk) {
-    const double work = steps * cycles / 4 / 256 / 2.1e3;  // us, with the chip full
-    int best = 1;
-    double least = 0;
-    for (int p = 1; p <= 16 && (p == 1 || p * 4 <= walk); ++p) {
-        const double t = work / std::min(1.0, workgroups * p / full) + (p > 1 ? 4 + p * bytes / 3.5e6 : 0);
-        if (p == 1 || t < least) {
-            best = p;
-            least = t;
-        }
-    }
-    return best;
-}
 struct WsLayout {
     int q_slots, k_slots, q_parts, k_parts;
     size_t aux, part_q, part_k, part_v, part_bias, total;
@@ -527,13 +504,11 @@ WsLayout layout(const AttnArgs &a, int d) {
     const int64_t rows = (int64_t)a.n_q * a.group;
     w.q_slots = (int)(rows / 128 + a.n_seq);
     w.k_slots = a.n_k / 128 + a.n_seq;
-    // walk steps of single wavefronts (32 x 32): those of an average sequence, half of them where causal
-    const double steps = (double)rows * a.h_kv / 32 * a.n_k / a.n_seq / 32 * (a.causal && a.n_q == a.n_k ? 0.5 : 1.0);
-    const int full = d == 32 ? 1024 : 512;
+    const double steps = walk_steps(a), full = full_chip(d);
     w.q_parts = best_parts(steps, d == 32 ? 450 : d == 64 ? 600 : 1050, ((double)rows / 128 + 1) * a.h_kv, full, (double)a.n_q * a.h_q * d * 8,
-                           (int64_t)a.n_k / a.n_seq / 32);
+                           (int64_t)a.n_k / a.n_seq / 32, (int64_t)w.q_slots * a.h_kv);
     w.k_parts = best_parts(steps, d == 32 ? 600 : d == 64 ? 800 : 1400, ((double)a.n_k / 128 + 1) * a.h_kv, full, (double)a.n_k * a.h_kv * d * 16,
-                           rows / a.n_seq / 32);
+                           rows / a.n_seq / 32, (int64_t)w.k_slots * a.h_kv);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -561,18 +536,17 @@ lsrm_status launch_backward_d(AttnArgs a, void *ws, hipStream_t st) {
         a.part_v = reinterpret_cast<float *>(base + w.part_v);
         a.part_bias = a.dbias != nullptr ? reinterpret_cast<float *>(base + w.part_bias) : nullptr;
         const int n_tab = bias_lds_floats(a) * 4;
-        a.n_slots = w.q_slots;
         a.parts = w.q_parts;
         lsrm_status rc = launch_attn(bias ? &attn_dq_kernel<D, true> : &attn_dq_kernel<D, false>, (int64_t)w.q_slots * a.h_kv * w.q_parts, 256,
                                      kDqLds<D> + n_tab, a, st);
         if (rc != LSRM_OK) return rc;
-        if (w.q_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, true>, (int64_t)(a.n_q / 128 + a.n_seq) * a.h_q, 256, 0, a, st)) != LSRM_OK) return rc;
+        if (w.q_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, true>, ((int64_t)a.n_q / (2048 / D) + a.n_seq) * a.h_q, 256, 0, a, st)) != LSRM_OK) return rc;
         a.parts = w.k_parts;
         rc = launch_attn(bias ? &attn_dkv_kernel<D, true> : &attn_dkv_kernel<D, false>, (int64_t)w.k_slots * a.h_kv * w.k_parts, 256,
                          kDkvLds<D> + kDkvValues<D> + (bias ? n_tab + 32 + (a.dbias != nullptr ? 16 * a.tab + 4 * Skew<kSkew<D>>::BYTES : 0) : 0), a, st);
         if (rc != LSRM_OK) return rc;
         a.n_slots = w.k_slots * w.k_parts;  // (of the bias' sums)
-        if (w.k_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, false>, (int64_t)w.k_slots * a.h_kv, 256, 0, a, st)) != LSRM_OK) return rc;
+        if (w.k_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, false>, ((int64_t)a.n_k / (2048 / D) + a.n_seq) * a.h_kv * 2, 256, 0, a, st)) != LSRM_OK) return rc;
     } else {
         a.n_slots = 0;
     }

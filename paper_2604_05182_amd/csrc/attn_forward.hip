@@ -138,15 +138,17 @@ constexpr int kStage = 64;  // keys per stage
 template <int D>
 constexpr int kForwardLds = 2 * kStage * 2 * AttnGeo<D>::ROW;
 
-template <int D, bool BIAS, bool LSE>
+// SPLIT: the keys are cut into a.parts parts, of which sums are left for attn_join_rows.
+template <int D, bool BIAS, bool LSE, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
     using G = AttnGeo<D>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
-    const int head_kv = blockIdx.x % a.h_kv;
+    const int head_kv = blockIdx.x % a.h_kv, place = blockIdx.x / a.h_kv;
+    const int part = SPLIT ? uniform(place % a.parts) : 0;
     int tile, seq;
     Sequence s;
-    if (!find_tile<false>(a, a.group, 128, blockIdx.x / a.h_kv, s, tile, seq)) return;
+    if (!find_tile<false>(a, a.group, 128, SPLIT ? uniform(place / a.parts) : place, s, tile, seq)) return;
     const int slot_rows = s.q_slot * a.group;
     if (a.causal) tile = (slot_rows - 1) / 128 - tile;  // the last rows, which see most keys, first
     const int v0 = tile * 128;
@@ -156,7 +158,12 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
         const int last = uniform((unsigned)min(v0 + 127, n_rows - 1) / (unsigned)a.group);
         keys = a.causal ? min(max(last + s.shift + 1, 0), s.n_k) : s.n_k;
     }
-    const int n_st = (keys + kStage - 1) / kStage;
+    int n_st = (keys + kStage - 1) / kStage, st_begin = 0;
+    if (SPLIT) {
+        const int per = uniform((n_st + a.parts - 1) / a.parts);
+        st_begin = part * per;
+        n_st = min(st_begin + per, n_st);
+    }
     const char *kb = reinterpret_cast<const char *>(a.k + s.k0 * a.ks[0] + head_kv * a.ks[1]);
     const char *vb = reinterpret_cast<const char *>(a.v + s.k0 * a.vs[0] + head_kv * a.vs[1]);
     const uint32_t k_row = (uint32_t)a.ks[0] * 2, v_row = (uint32_t)a.vs[0] * 2;
@@ -166,7 +173,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
         copy_rows<D, kStage, 4>(kb + (uint64_t)j0 * k_row, k_row, keys - j0, at, wave, c);
         copy_rows<D, kStage, 4>(vb + (uint64_t)j0 * v_row, v_row, keys - j0, at + kStage * G::ROW, wave, c);
     };
-    if (n_st > 0) copy_stage(0, lds);
+    if (st_begin < n_st) copy_stage(st_begin, lds);
     float *tab = reinterpret_cast<float *>(lds + kForwardLds<D>);
     if (BIAS) expand_bias(a, head_kv, tab, 256);
     Rows<D, BIAS> r;
@@ -183,7 +190,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
                 attend<D, BIAS, LSE>(a, r, at + h * G::TILE, at + (kStage + 32 * h) * G::ROW, t, st * kStage + 32 * h, hh);
     };
     constexpr int STAGE = 2 * kStage * G::ROW;
-    for (int st = 0; st < n_st; st += 2) {
+    for (int st = st_begin; st < n_st; st += 2) {
         stage(st, lds, lds + STAGE);
         if (st + 1 < n_st) stage(st + 1, lds + STAGE, lds);
     }
@@ -193,6 +200,20 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
     const float l = half_sum(r.l), inv = l > 0.f || l != l ? 1.0f / l : 0.f;
     const int row = v0 + wave * 32 + (lane & 31);
     const bool live = row < n_rows;
+    if (SPLIT) {
+        if (row >= slot_rows) return;
+        const int tok = (unsigned)row / (unsigned)a.group;
+        const int64_t at = ((int64_t)part * a.n_q + s.q0 + tok) * a.h_q + head_kv * a.group + row - tok * a.group;
+        if (hh == 0) a.part_ml[at] = make_float2(r.m * (BIAS ? 1.0f : a.sl2), live ? l : 0.f);
+        float *to = a.part + at * D + 4 * hh;
+#pragma unroll
+        for (int dt = 0; dt < G::ND; ++dt)
+#pragma unroll
+            for (int gq = 0; gq < 4; ++gq)
+                *reinterpret_cast<f32x4 *>(to + 32 * dt + 8 * gq) =
+                    f32x4{r.o[dt][4 * gq], r.o[dt][4 * gq + 1], r.o[dt][4 * gq + 2], r.o[dt][4 * gq + 3]};
+        return;
+    }
     store_query_rows<D>(a, s, head_kv, v0 + wave * 32, slot_rows, r.o, inv, live, lds + wave * 32 * G::OUT_ROW, a.out, a.os, lane);
     if (LSE && hh == 0 && row < slot_rows) {
         const int tok = (unsigned)row / (unsigned)a.group, g = row - tok * a.group;
@@ -205,9 +226,6 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
 // Where there are too few tiles of rows to fill the chip, the keys are cut into parts too: a unit is (tile of 32 rows, part), a part
 // the same number of keys in all sequences, so that sequences of different lengths cost what they hold.  Every workgroup works that
 // number out from the lengths (there is no one to ask: offsets and lengths are in device memory and the host must not wait).
-struct Plan {
-    int chunk;  // keys per part
-};
 __device__ __forceinline__ int row_tiles(const AttnArgs &a, const Sequence &s) { return (s.q_slot * a.group + kFewRows - 1) / kFewRows; }
 __device__ __forceinline__ int parts_of(const Sequence &s, int chunk) { return max(1, (s.n_k + chunk - 1) / chunk); }
 __device__ __forceinline__ int part_keys(const AttnArgs &a) {
@@ -443,50 +461,123 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
     }
 }
 
-enum Way { MANY, FEW, FEW_SPLIT };
-// How a forward call is worked on.  slots32: tiles of 32 rows at most.
-Way forward_way(const AttnArgs &a, int64_t *slots32) {
-    const int64_t rows = (int64_t)a.n_q * a.group;
-    *slots32 = rows / kFewRows + a.n_seq;
-    if (rows >= (int64_t)64 * a.n_seq && (rows / 128 + 1) * a.h_kv >= 256) return MANY;
-    if (*slots32 * a.h_kv >= 512) return rows >= (int64_t)64 * a.n_seq ? MANY : FEW;
-    return a.n_k / a.n_seq <= 1024 ? FEW : FEW_SPLIT;
+// Joins the parts of attn_forward_kernel: up to 2048 / d queries of a sequence's slot, one head to a workgroup, eight channels to a thread.
+template <int D>
+__global__ __launch_bounds__(256) void attn_join_rows(AttnArgs a) {
+    constexpr int CH = D / 8, ROWS = 256 / CH;
+    const int head = blockIdx.x % a.h_q;
+    int tile, seq;
+    Sequence s;
+    if (!find_tile<false>(a, 1, ROWS, blockIdx.x / a.h_q, s, tile, seq)) return;
+    const int r = tile * ROWS + threadIdx.x / CH, c0 = threadIdx.x % CH * 8;
+    if (r >= s.q_slot) return;
+    const int64_t at = (int64_t)(s.q0 + r) * a.h_q + head, step = (int64_t)a.n_q * a.h_q;
+    float m2 = kMinusHuge, sum = 0.f, x[8] = {};
+    for (int p = 0; p < a.parts; ++p) m2 = fmaxf(m2, a.part_ml[at + p * step].x);
+#pragma unroll 4
+    for (int p = 0; p < a.parts; ++p) {
+        const float2 ml = a.part_ml[at + p * step];
+        const float f = __builtin_amdgcn_exp2f(ml.x - m2);
+        sum += f * ml.y;
+        const f32x4 *from = reinterpret_cast<const f32x4 *>(a.part + (at + p * step) * D + c0);
+        const f32x4 y = from[0], z = from[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] += f * y[i];
+            x[4 + i] += f * z[i];
+        }
+    }
+    const int head_kv = head / a.group;
+    store_channels<8>(a, s, head_kv, r * a.group + head - head_kv * a.group, c0, x, m2, sum);
 }
-// Units that the keys are cut into, per key/value head: two workgroups for every CU, or twice the tiles where there are many.
-int unit_cap(const AttnArgs &a, int64_t slots32) { return (int)std::max<int64_t>(2 * slots32, 512 / a.h_kv); }
+
+// How a forward call is worked on.  Sequences of 64 and more rows (queries times heads of a group) go to workgroups of 128 rows, whose
+// keys are cut into parts where there are few of them; shorter ones to workgroups of 32 rows, whose keys are cut where there are few of them and
+// the keys are long enough that the second launch does not cost more than it saves (4 streams of 513 keys: 11.1 us cut, 6.8 whole).
+enum Way { MANY, FEW, FEW_SPLIT };
+struct Plan {
+    Way way;
+    int64_t slots32;  // tiles of 32 rows at most
+    int parts;        // MANY
+    int unit_cap;     // FEW_SPLIT: units that the keys are cut into, per key/value head: two workgroups for every CU, or twice the tiles where
+                      // there are many
+    size_t part, part_ml, total;  // workspace
+};
+Plan forward_plan(const AttnArgs &a, int d) {
+    Plan p{};
+    const int64_t rows = (int64_t)a.n_q * a.group;
+    p.slots32 = rows / kFewRows + a.n_seq;
+    p.parts = 1;
+    if (rows >= (int64_t)64 * a.n_seq) {
+        p.way = MANY;
+        p.parts = best_parts(walk_steps(a), d == 32 ? 380 : d == 64 ? 540 : 700, ((double)rows / 128 + 1) * a.h_kv, full_chip(d),
+                             (double)a.n_q * a.h_q * (d + 2) * 8, (int64_t)a.n_k / a.n_seq / 32, (rows / 128 + a.n_seq) * a.h_kv);
+        if (p.parts > 1) {
+            p.part_ml = align_up((size_t)p.parts * a.n_q * a.h_q * d * 4, 256);
+            p.total = p.part_ml + (size_t)p.parts * a.n_q * a.h_q * 8;
+        }
+    } else if (p.slots32 * a.h_kv >= 256 || a.n_k / a.n_seq <= 1024) {
+        p.way = FEW;
+    } else {
+        p.way = FEW_SPLIT;
+        p.unit_cap = (int)std::max<int64_t>(2 * p.slots32, 512 / a.h_kv);
+        p.total = (size_t)p.unit_cap * a.h_kv * kFewRows * (d + 2) * 4;
+    }
+    return p;
+}
+
+template <int D, bool SPLIT>
+lsrm_status launch_many(const AttnArgs &a, int64_t grid, int lds, hipStream_t st) {
+    const bool lse = a.lse != nullptr || SPLIT;
+    auto kernel = a.n_buckets > 0 ? (lse ? &attn_forward_kernel<D, true, true, SPLIT> : &attn_forward_kernel<D, true, SPLIT, SPLIT>)
+                                  : (lse ? &attn_forward_kernel<D, false, true, SPLIT> : &attn_forward_kernel<D, false, SPLIT, SPLIT>);
+    return launch_attn(kernel, grid, 256, lds, a, st);
+}
 
 template <int D>
 lsrm_status launch_forward_d(AttnArgs a, void *ws, hipStream_t st) {
-    int64_t slots32;
-    const Way way = forward_way(a, &slots32);
+    const Plan p = forward_plan(a, D);
     const int tab = bias_lds_floats(a) * 4;
     const bool bias = a.n_buckets > 0;
-    if (way == MANY) {
-        a.n_slots = (int)((int64_t)a.n_q * a.group / 128 + a.n_seq);
-        const bool lse = a.lse != nullptr;
-        auto kernel = bias ? (lse ? &attn_forward_kernel<D, true, true> : &attn_forward_kernel<D, true, false>)
-                           : (lse ? &attn_forward_kernel<D, false, true> : &attn_forward_kernel<D, false, false>);
-        return launch_attn(kernel, (int64_t)a.n_slots * a.h_kv, 256, kForwardLds<D> + tab, a, st);
+    if (p.way == MANY) {
+        const int64_t grid = ((int64_t)a.n_q * a.group / 128 + a.n_seq) * a.h_kv * p.parts;
+        a.parts = p.parts;
+        if (p.parts == 1) return launch_many<D, false>(a, grid, kForwardLds<D> + tab, st);
+        a.part = static_cast<float *>(ws);
+        a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + p.part_ml);
+        const lsrm_status rc = launch_many<D, true>(a, grid, kForwardLds<D> + tab, st);
+        if (rc != LSRM_OK) return rc;
+        return launch_attn(&attn_join_rows<D>, ((int64_t)a.n_q / (2048 / D) + a.n_seq) * a.h_q, 256, 0, a, st);
     }
-    const int64_t n_tiles = slots32 * a.h_kv;
-    if (way == FEW)
+    const int64_t n_tiles = p.slots32 * a.h_kv;
+    if (p.way == FEW)
         return bias ? launch_attn(&attn_few_kernel<D, true, false>, n_tiles, 64 * kFewWaves<D, true>, kFewLds<D, true> + tab, a, st)
                     : launch_attn(&attn_few_kernel<D, false, false>, n_tiles, 64 * kFewWaves<D, false>, kFewLds<D, false>, a, st);
-    a.unit_cap = unit_cap(a, slots32);
+    a.unit_cap = p.unit_cap;
     a.part = static_cast<float *>(ws);
     lsrm_status rc = launch_attn(bias ? &attn_few_kernel<D, true, true> : &attn_few_kernel<D, false, true>, (int64_t)a.unit_cap * a.h_kv,
                                  64 * kFewWaves<D, true>, kFewLds<D, true> + tab, a, st);
     if (rc != LSRM_OK) return rc;
-    return launch_attn(&attn_join_kernel<D>, slots32 * a.h_kv * kJoinWays, 256, 0, a, st);
+    return launch_attn(&attn_join_kernel<D>, n_tiles * kJoinWays, 256, 0, a, st);
 }
 
 }  // namespace
 
-size_t attn_forward_ws_bytes(const AttnArgs &a, int d) {
-    int64_t slots32;
-    if (a.n_seq == 0 || a.n_q == 0 || forward_way(a, &slots32) != FEW_SPLIT) return 0;
-    return (size_t)unit_cap(a, slots32) * a.h_kv * kFewRows * (d + 2) * 4;
+int best_parts(double steps, double cycles, double workgroups, double full, double bytes, int64_t walk, int64_t grid) {
+    const double work = steps * cycles / 4 / 256 / 2.1e3;  // us, with the chip full
+    int best = 1;
+    double least = 0;
+    for (int p = 1; p <= 16 && (p == 1 || (p * 4 <= walk && p * grid <= 1 << 23)); ++p) {
+        const double t = work / std::min(1.0, workgroups * p / full) + (p > 1 ? 4 + p * bytes / 3.5e6 : 0);
+        if (p == 1 || t < least) {
+            best = p;
+            least = t;
+        }
+    }
+    return best;
 }
+
+size_t attn_forward_ws_bytes(const AttnArgs &a, int d) { return a.n_seq == 0 || a.n_q == 0 ? 0 : forward_plan(a, d).total; }
 
 lsrm_status launch_attn_forward(AttnArgs a, int d, void *ws, hipStream_t st) {
     switch (d) {

@@ -27,10 +27,11 @@ struct AttnArgs {
     const int32_t *q_off, *k_off, *q_len, *k_len;
     int64_t qs[2], ks[2], vs[2], os[2];  // {row, head} strides in elements
     int n_q, n_k, n_seq, h_q, h_kv, group, causal;
-    int n_slots;           // tiles of query rows of all sequences at most (see find_tile)
+    int n_slots;           // backward: workgroups that leave sums of the bias' gradient
     int unit_cap;          // forward of few rows: units of all sequences at most
-    int parts;             // backward: parts that a walk is cut into
-    float *part;           // forward of few rows: sums of the parts
+    int parts;             // parts that the walk of a workgroup is cut into
+    float *part;           // forward: sums of the parts
+    float2 *part_ml;       // forward of many rows: their maxima and sums of exponentials
     float2 *aux;           // backward: [h_q][n_q] {lse log2e (+inf for a query without keys), -D}, one such for each part of the dQ walks
     float *part_q, *part_k, *part_v, *part_bias;
     int n_buckets, b0, b_last;  // of the bias (0: none), first and last bound
@@ -325,6 +326,20 @@ __device__ __forceinline__ void store_query_rows(const AttnArgs &a, const Sequen
         }
     }
 }
+
+// Where there are few workgroups, walks are cut into parts, of which fp32 sums are added up afterwards.  How many is a trade between walks
+// that leave the chip empty and sums that are written and read; by what both take (one walk step of a wavefront: `cycles`, the chip
+// full from `full` workgroups on; 3.5 bytes of sums a nanosecond, and 4 us for the launch):
+//   T(parts) = steps / min(1, workgroups parts / full) + (parts > 1) (4 us + parts bytes / 3.5 TB/s)
+// Always 512 workgroups instead: 32 heads of 32 on 2, 6372 tokens 450 -> 390 us a training step.
+// walk: steps of an average walk (a part has four at least); grid: workgroups that are launched for each part.
+int best_parts(double steps, double cycles, double workgroups, double full, double bytes, int64_t walk, int64_t grid);
+// walk steps of single wavefronts (32 x 32): those of average sequences, half of them where causal
+inline double walk_steps(const AttnArgs &a) {
+    return (double)a.n_q * a.group * a.h_kv / 32 * a.n_k / a.n_seq / 32 * (a.causal && a.n_q == a.n_k ? 0.5 : 1.0);
+}
+// workgroups that fill the chip
+inline int full_chip(int d) { return d == 32 ? 1024 : 512; }
 
 template <typename F>
 lsrm_status launch_attn(F kernel, int64_t grid, int threads, int lds, const AttnArgs &a, hipStream_t st) {
