@@ -491,9 +491,11 @@ __global__ __launch_bounds__(256) void attn_join_rows(AttnArgs a) {
     store_channels<8>(a, s, head_kv, r * a.group + head - head_kv * a.group, c0, x, m2, sum);
 }
 
-// How a forward call is worked on.  Sequences of 64 and more rows (queries times heads of a group) go to workgroups of 128 rows, whose
-// keys are cut into parts where there are few of them; shorter ones to workgroups of 32 rows, whose keys are cut where there are few of them and
-// the keys are long enough that the second launch does not cost more than it saves (4 streams of 513 keys: 11.1 us cut, 6.8 whole).
+// How a forward call is worked on.  FEW: workgroups of 32 rows, whose wavefronts take turns at the keys: where these are all on the chip at
+// the same time and the keys are short, a call takes as long as the fewest steps behind each other (5 sequences of up to 130 tokens, 4
+// heads of 64 with a bias: 7.3 us, 9.4 in workgroups of 128 rows).  MANY: sequences of 64 and more rows (queries times heads of a group)
+// in workgroups of 128, whose keys are cut into parts where there are few of them.  Others are cut for long keys, where the second launch
+// does not cost more than it saves (4 streams of up to 513 keys: 11.1 us cut, 6.8 whole).
 enum Way { MANY, FEW, FEW_SPLIT };
 struct Plan {
     Way way;
@@ -508,7 +510,10 @@ Plan forward_plan(const AttnArgs &a, int d) {
     const int64_t rows = (int64_t)a.n_q * a.group;
     p.slots32 = rows / kFewRows + a.n_seq;
     p.parts = 1;
-    if (rows >= (int64_t)64 * a.n_seq) {
+    const bool small = p.slots32 * a.h_kv <= (d == 32 ? 512 : 256), short_keys = a.n_k / a.n_seq <= 1024;
+    if (small && short_keys) {
+        p.way = FEW;
+    } else if (rows >= (int64_t)64 * a.n_seq) {
         p.way = MANY;
         p.parts = best_parts(walk_steps(a), d == 32 ? 380 : d == 64 ? 540 : 700, ((double)rows / 128 + 1) * a.h_kv, full_chip(d),
                              (double)a.n_q * a.h_q * (d + 2) * 8, (int64_t)a.n_k / a.n_seq / 32, (rows / 128 + a.n_seq) * a.h_kv);
@@ -516,7 +521,7 @@ Plan forward_plan(const AttnArgs &a, int d) {
             p.part_ml = align_up((size_t)p.parts * a.n_q * a.h_q * d * 4, 256);
             p.total = p.part_ml + (size_t)p.parts * a.n_q * a.h_q * 8;
         }
-    } else if (p.slots32 * a.h_kv >= 256 || a.n_k / a.n_seq <= 1024) {
+    } else if (p.slots32 * a.h_kv >= 256 || short_keys) {
         p.way = FEW;
     } else {
         p.way = FEW_SPLIT;
