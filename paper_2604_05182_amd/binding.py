@@ -267,7 +267,8 @@ def make_attn_params(q, k, v, q_offsets, k_offsets=None, q_lens=None, k_lens=Non
     p.d_q_lens, p.d_k_lens = _int32("q_lens", q_lens, n_seq), _int32("k_lens", k_lens, n_seq)
     p._keepalive = (q_offsets, k_offsets, q_lens, k_lens)
     p.q_stride[:], p.k_stride[:], p.v_stride[:], p.o_stride[:] = q_st, k_st, v_st, o_st
-    p._of = {"q": ((n_q, h_q, d), q_st), "k": ((n_k, h_kv, d), k_st), "v": ((n_k, h_kv, d), v_st), "o": ((n_q, h_q, d), o_st)}
+    p._of = {"q": ((n_q, h_q, d), q_st + (1,)), "k": ((n_k, h_kv, d), k_st + (1,)), "v": ((n_k, h_kv, d), v_st + (1,)),
+             "o": ((n_q, h_q, d), o_st + (1,))}
     if bucket_bounds is not None:
         arr = (ctypes.c_int32 * max(len(bucket_bounds), 1))(*[int(x) for x in bucket_bounds])
         p._bounds = arr
@@ -280,6 +281,8 @@ def _rows(p, which, name, t):
     """Pointer of a tensor that has to be laid out as the description says."""
     shape, stride = p._of[which]
     st = t.stride()
+    if t.shape == shape and st == stride and t.dtype is torch.bfloat16 and t.is_cuda:
+        return t.data_ptr()
     if (t.shape != shape or t.dtype is not torch.bfloat16 or not t.is_cuda or (shape[0] > 1 and st[0] != stride[0]) or
             (shape[1] > 1 and st[1] != stride[1]) or st[2] != 1):
         raise ValueError(f"{name}: bf16 {shape} with strides {stride} on the GPU expected, got {t.dtype} {tuple(t.shape)} {st} {t.device}")

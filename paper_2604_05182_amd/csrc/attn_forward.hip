@@ -228,57 +228,61 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
 // number out from the lengths (there is no one to ask: offsets and lengths are in device memory and the host must not wait).
 __device__ __forceinline__ int row_tiles(const AttnArgs &a, const Sequence &s) { return (s.q_slot * a.group + kFewRows - 1) / kFewRows; }
 __device__ __forceinline__ int parts_of(const Sequence &s, int chunk) { return max(1, (s.n_k + chunk - 1) / chunk); }
-__device__ __forceinline__ int part_keys(const AttnArgs &a) {
+// keys of a part, where the sequences have `tiles` tiles that attend `keys` keys in all:
+// sum over tiles of ceil(keys / chunk) <= keys / chunk + tiles <= unit_cap
+__device__ __forceinline__ int part_keys(const AttnArgs &a, int64_t keys, int tiles) {
+    const int room = max(a.unit_cap - tiles, 1);
+    return uniform(max(256, (int)((keys + room - 1) / room + 127) / 128 * 128));
+}
+// The sequence of number x -- of a unit (UNITS), or of a tile of rows -- what is left of x within it, and the units of the sequences before.
+// False if there is none.  A lane holds one sequence; up to 64 of them are loaded once.
+template <bool UNITS>
+__device__ __forceinline__ bool find_unit(const AttnArgs &a, int x, Sequence &s, int &within, int &chunk, int &units_before) {
     const int lane = threadIdx.x & 63;
+    Sequence mine = {};
     int64_t keys = 0;
     int tiles = 0;
     for (int i = lane; i < a.n_seq; i += 64) {
-        const Sequence s = load_sequence(a, i);
-        tiles += row_tiles(a, s);
-        keys += (int64_t)row_tiles(a, s) * s.n_k;
+        mine = load_sequence(a, i);
+        tiles += row_tiles(a, mine);
+        keys += (int64_t)row_tiles(a, mine) * mine.n_k;
     }
-    for (int x = 32; x > 0; x /= 2) {
-        keys += __shfl_xor(keys, x);
-        tiles += __shfl_xor(tiles, x);
+    for (int y = 32; y > 0; y /= 2) {
+        keys += __shfl_xor(keys, y);
+        tiles += __shfl_xor(tiles, y);
     }
-    // sum over tiles of ceil(keys / chunk) <= keys / chunk + tiles <= unit_cap
-    const int room = max(a.unit_cap - tiles, 1);
-    return __builtin_amdgcn_readfirstlane(max(256, (int)((keys + room - 1) / room + 127) / 128 * 128));
-}
-// units of the sequences before s
-__device__ __forceinline__ int units_before(const AttnArgs &a, int seq, int chunk) {
-    int n = 0;
-    for (int i = threadIdx.x & 63; i < seq; i += 64) {
-        const Sequence s = load_sequence(a, i);
-        n += row_tiles(a, s) * parts_of(s, chunk);
-    }
-    for (int x = 32; x > 0; x /= 2) n += __shfl_xor(n, x);
-    return __builtin_amdgcn_readfirstlane(n);
-}
-// sequence of a unit (n_seq if there is none) and the unit's number within it
-__device__ __forceinline__ int unit_sequence(const AttnArgs &a, int unit, int chunk, int *within) {
-    const int lane = threadIdx.x & 63;
-    int base = 0;
+    chunk = part_keys(a, keys, tiles);
+    int base = 0, units = 0;  // of the sequences before these 64: numbers, units
     for (int i0 = 0; i0 < a.n_seq; i0 += 64) {
-        int n = 0;
-        if (i0 + lane < a.n_seq) {
-            const Sequence s = load_sequence(a, i0 + lane);
-            n = row_tiles(a, s) * parts_of(s, chunk);
+        const bool any = i0 + lane < a.n_seq;
+        if (a.n_seq > 64 && any) mine = load_sequence(a, i0 + lane);
+        const int u = any ? row_tiles(a, mine) * parts_of(mine, chunk) : 0, n = UNITS ? u : any ? row_tiles(a, mine) : 0;
+        int upto = n, u_upto = u;
+        for (int y = 1; y < 64; y *= 2) {
+            const int b = __shfl_up(upto, y), c = __shfl_up(u_upto, y);
+            if (lane >= y) {
+                upto += b;
+                u_upto += c;
+            }
         }
-        int upto = n;
-        for (int x = 1; x < 64; x *= 2) {
-            const int y = __shfl_up(upto, x);
-            if (lane >= x) upto += y;
-        }
-        const uint64_t found = __builtin_amdgcn_ballot_w64(unit < base + upto);
+        const uint64_t found = __builtin_amdgcn_ballot_w64(n > 0 && x < base + upto);
         if (found != 0) {
             const int at = __builtin_ctzll(found);
-            *within = __builtin_amdgcn_readfirstlane(unit - base - __shfl(upto - n, at));
-            return i0 + at;
+            within = x - base - __builtin_amdgcn_readlane(upto - n, at);
+            units_before = units + __builtin_amdgcn_readlane(u_upto - u, at);
+            s.q0 = __builtin_amdgcn_readlane(mine.q0, at);
+            s.n_q = __builtin_amdgcn_readlane(mine.n_q, at);
+            s.q_slot = __builtin_amdgcn_readlane(mine.q_slot, at);
+            s.k0 = __builtin_amdgcn_readlane(mine.k0, at);
+            s.n_k = __builtin_amdgcn_readlane(mine.n_k, at);
+            s.k_slot = __builtin_amdgcn_readlane(mine.k_slot, at);
+            s.shift = s.n_k - s.n_q;
+            return true;
         }
-        base += __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+        base += __builtin_amdgcn_readlane(upto, 63);
+        units += __builtin_amdgcn_readlane(u_upto, 63);
     }
-    return a.n_seq;
+    return false;
 }
 
 // Wavefronts of a workgroup.  Each has a ring of two slots (a K and a V tile) of its own.  Where the keys are cut, two workgroups share a CU, so
@@ -319,20 +323,15 @@ __global__ __launch_bounds__((64 * kFewWaves<D, SPLIT || BIAS>), 1) void attn_fe
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv, unit = blockIdx.x / a.h_kv;
-    int tile, seq, part = 0, n_parts = 1, chunk = 0;
+    int tile, part = 0, n_parts = 1, chunk = 0, unused;
     Sequence s;
     if (SPLIT) {
-        chunk = part_keys(a);
-        seq = uniform(unit_sequence(a, unit, chunk, &tile));
-        if (seq >= a.n_seq) return;
-        s = load_sequence(a, seq);
-    } else if (!find_tile<false>(a, a.group, kFewRows, unit, s, tile, seq)) {
-        return;
-    }
-    if (SPLIT) {
+        if (!find_unit<true>(a, unit, s, tile, chunk, unused)) return;
         n_parts = uniform(parts_of(s, chunk));
         part = uniform(tile % n_parts);
         tile = uniform(tile / n_parts);
+    } else if (!find_tile<false>(a, a.group, kFewRows, unit, s, tile, unused)) {
+        return;
     }
     const int v0 = tile * kFewRows, slot_rows = s.q_slot * a.group;
     if (v0 < 0 || v0 >= slot_rows) return;
@@ -422,14 +421,12 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
     __shared__ f32x4 sums[GROUPS][LANES];
     __shared__ float part_max[4], part_sum[4];
     const int way = blockIdx.x % kJoinWays, head_kv = blockIdx.x / kJoinWays % a.h_kv, slot = blockIdx.x / kJoinWays / a.h_kv;
-    int tile, seq;
+    int tile, chunk, unit;
     Sequence s;
-    if (!find_tile<false>(a, a.group, kFewRows, slot, s, tile, seq)) return;
-    const int slot_rows = s.q_slot * a.group;
-    if (tile * kFewRows + way >= slot_rows) return;
-    const int chunk = part_keys(a), n_parts = parts_of(s, chunk);
-    if (n_parts == 1) return;
-    const int unit = units_before(a, seq, chunk) + tile * n_parts;
+    if (!find_unit<false>(a, slot, s, tile, chunk, unit)) return;
+    const int slot_rows = s.q_slot * a.group, n_parts = parts_of(s, chunk);
+    if (n_parts == 1 || tile * kFewRows + way >= slot_rows) return;
+    unit += tile * n_parts;
     if (unit < 0 || n_parts > a.unit_cap - unit) return;  // (of offsets that do not ascend)
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, wave = threadIdx.x / 64;
     const float *from = a.part + ((int64_t)unit * a.h_kv + head_kv) * kPartFloats<D>;
