@@ -83,36 +83,29 @@ __device__ __forceinline__ void mask_scores(const Rows<D, BIAS> &r, f32x16 &s, i
     }
 }
 
-// The exponentials of a tile's scores, as the next product's operand, and their sum.  The sum is of the rounded values, two to an
-// instruction, where the log-sum-exp is not wanted: normalised by what was summed up, the outputs are a little nearer to the exact ones then.
-template <bool EXACT_SUM>
+// The exponentials of a tile's scores, as the next product's operand; returns their sum.
 __device__ __forceinline__ float exponentials(const f32x16 &s, float sl, float mc, BFrag (&b)[2]) {
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const float x = __builtin_amdgcn_exp2f(s[2 * k] * sl - mc), y = __builtin_amdgcn_exp2f(s[2 * k + 1] * sl - mc);
-        const uint32_t xy = pack_bf16(x, y);
-        b[k / 4].u[k % 4] = xy;
-        if (EXACT_SUM) {
-            sum += x;
-            sum += y;
-        } else {
-            sum = add_pair(xy, sum);
-        }
+        b[k / 4].u[k % 4] = pack_bf16(x, y);
+        sum += x;
+        sum += y;
     }
     return sum;
 }
 
 // One tile of 32 keys from key j0 of the sequence on.  Where a sum exceeds the limit, the running maximum is raised, what was summed so
 // far rescaled, and the tile's exponentials done again.
-template <int D, bool BIAS, bool EXACT_SUM>
+template <int D, bool BIAS>
 __device__ __forceinline__ void attend(const AttnArgs &a, Rows<D, BIAS> &r, const char *kt, const char *vt, const TileLane<D> &t, int j0, int hh) {
     f32x16 s = mfma_rows<D>(splat(0.f), kt, t, r.q);
     const float sl = BIAS ? 1.0f : a.sl2;
     if (BIAS) add_bias<D, BIAS>(a, r, s, j0, hh);
     mask_scores<D, BIAS>(r, s, j0, hh);
     BFrag b[2];
-    float sum = exponentials<EXACT_SUM>(s, sl, r.m * sl, b);
+    float sum = exponentials(s, sl, r.m * sl, b);
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kSumLimit)) != 0, 0)) {
         mfma_settle();  // the accumulators of the tile before may be in flight
         float mx = s[0];
@@ -127,7 +120,7 @@ __device__ __forceinline__ void attend(const AttnArgs &a, Rows<D, BIAS> &r, cons
         for (int dt = 0; dt < AttnGeo<D>::ND; ++dt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) asm volatile("v_mul_f32 %0, %1, %0" : "+v"(r.o[dt][i]) : "v"(alpha));
-        sum = exponentials<EXACT_SUM>(s, sl, m_new * sl, b);
+        sum = exponentials(s, sl, m_new * sl, b);
     }
     r.l += sum;
     mfma_transposed<D>(r.o, vt, t, b);
@@ -139,7 +132,7 @@ template <int D>
 constexpr int kForwardLds = 2 * kStage * 2 * AttnGeo<D>::ROW;
 
 // SPLIT: the keys are cut into a.parts parts, of which sums are left for attn_join_rows.
-template <int D, bool BIAS, bool LSE, bool SPLIT>
+template <int D, bool BIAS, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
     using G = AttnGeo<D>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -187,7 +180,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
             if (st * kStage + 32 * h < r.lim_max)
-                attend<D, BIAS, LSE>(a, r, at + h * G::TILE, at + (kStage + 32 * h) * G::ROW, t, st * kStage + 32 * h, hh);
+                attend<D, BIAS>(a, r, at + h * G::TILE, at + (kStage + 32 * h) * G::ROW, t, st * kStage + 32 * h, hh);
     };
     constexpr int STAGE = 2 * kStage * G::ROW;
     for (int st = st_begin; st < n_st; st += 2) {
@@ -215,7 +208,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
         return;
     }
     store_query_rows<D>(a, s, head_kv, v0 + wave * 32, slot_rows, r.o, inv, live, lds + wave * 32 * G::OUT_ROW, a.out, a.os, lane);
-    if (LSE && hh == 0 && row < slot_rows) {
+    if (a.lse != nullptr && hh == 0 && row < slot_rows) {
         const int tok = (unsigned)row / (unsigned)a.group, g = row - tok * a.group;
         a.lse[(int64_t)(s.q0 + tok) * a.h_q + head_kv * a.group + g] =
             live && inv != 0.f ? (r.m * (BIAS ? 1.0f : a.sl2) + __builtin_amdgcn_logf(l)) * kLn2 : -__builtin_inff();
@@ -365,7 +358,7 @@ __global__ __launch_bounds__((64 * kFewWaves<D, SPLIT || BIAS>), 1) void attn_fe
             wait_copies<0>();
         }
         const char *at = ring + slot * 2 * G::TILE;
-        attend<D, BIAS, true>(a, r, at, at + G::TILE, t, j0, hh);
+        attend<D, BIAS>(a, r, at, at + G::TILE, t, j0, hh);
     }
     // the wavefronts' sums meet in LDS
     mfma_settle();
@@ -528,14 +521,6 @@ Plan forward_plan(const AttnArgs &a, int d) {
     return p;
 }
 
-template <int D, bool SPLIT>
-lsrm_status launch_many(const AttnArgs &a, int64_t grid, int lds, hipStream_t st) {
-    const bool lse = a.lse != nullptr || SPLIT;
-    auto kernel = a.n_buckets > 0 ? (lse ? &attn_forward_kernel<D, true, true, SPLIT> : &attn_forward_kernel<D, true, SPLIT, SPLIT>)
-                                  : (lse ? &attn_forward_kernel<D, false, true, SPLIT> : &attn_forward_kernel<D, false, SPLIT, SPLIT>);
-    return launch_attn(kernel, grid, 256, lds, a, st);
-}
-
 template <int D>
 lsrm_status launch_forward_d(AttnArgs a, void *ws, hipStream_t st) {
     const Plan p = forward_plan(a, D);
@@ -544,10 +529,13 @@ lsrm_status launch_forward_d(AttnArgs a, void *ws, hipStream_t st) {
     if (p.way == MANY) {
         const int64_t grid = ((int64_t)a.n_q * a.group / 128 + a.n_seq) * a.h_kv * p.parts;
         a.parts = p.parts;
-        if (p.parts == 1) return launch_many<D, false>(a, grid, kForwardLds<D> + tab, st);
+        if (p.parts == 1)
+            return launch_attn(bias ? &attn_forward_kernel<D, true, false> : &attn_forward_kernel<D, false, false>, grid, 256,
+                               kForwardLds<D> + tab, a, st);
         a.part = static_cast<float *>(ws);
         a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + p.part_ml);
-        const lsrm_status rc = launch_many<D, true>(a, grid, kForwardLds<D> + tab, st);
+        const lsrm_status rc = launch_attn(bias ? &attn_forward_kernel<D, true, true> : &attn_forward_kernel<D, false, true>, grid, 256,
+                                           kForwardLds<D> + tab, a, st);
         if (rc != LSRM_OK) return rc;
         return launch_attn(&attn_join_rows<D>, ((int64_t)a.n_q / (2048 / D) + a.n_seq) * a.h_q, 256, 0, a, st);
     }

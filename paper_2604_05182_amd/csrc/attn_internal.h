@@ -259,11 +259,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     p[1] = (__bf16)b;
     return *reinterpret_cast<uint32_t *>(&p);
 }
-// sum + both values of a pair
-__device__ __forceinline__ float add_pair(uint32_t xy, float sum) {
-    const uint32_t ones = 0x3f803f80u;
-    return __builtin_amdgcn_fdot2_f32_bf16(*reinterpret_cast<const bf16x2 *>(&xy), *reinterpret_cast<const bf16x2 *>(&ones), sum, false);
-}
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 // accumulator tile -> the two B operands (16-row slabs) of the next contraction
