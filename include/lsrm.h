@@ -22,7 +22,7 @@
  *   - no global state apart from lsrm_route_blocks_static's address lookup; calls may come from any
  *     thread and any device may be current;
  *   - the library allocates no device memory: scratch comes from the caller
- *     (d_ws / ws_bytes, size from lsrm_workspace_bytes, 256-byte aligned), except in
+ *     (d_ws / ws_bytes, size from lsrm_workspace_bytes or lsrm_attn_workspace_bytes, 256-byte aligned), except in
  *     lsrm_route_blocks_static, which uses a fixed array inside the library;
  *   - nothing throws or aborts: the return value is LSRM_OK or a negative code,
  *     and on error no kernel has been launched.
@@ -349,7 +349,8 @@ typedef struct lsrm_attn_params {
 } lsrm_attn_params;
 
 /* Bytes of scratch for lsrm_attn_forward (LSRM_WS_FORWARD) or lsrm_attn_backward (LSRM_WS_BACKWARD); 0 on invalid
- * params, and where the call needs none. */
+ * params, and where the call needs none.  What it holds lives for one call: calls that may run at the same time (on two
+ * streams, in two graphs) need one each, calls behind each other can share. */
 size_t lsrm_attn_workspace_bytes(const lsrm_attn_params *p, int which_call);
 
 /*

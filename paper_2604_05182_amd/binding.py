@@ -238,7 +238,7 @@ def _layout(name, t, heads=None, d=None):
 def _int32(name, t, n):
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name}: contiguous int32 [{n}] on the GPU expected")
     return t.data_ptr()
 
@@ -260,6 +260,9 @@ def make_attn_params(q, k, v, q_offsets, k_offsets=None, q_lens=None, k_lens=Non
         o_shape, o_st = _layout("out", out)
         if o_shape != (n_q, h_q, d):
             raise ValueError(f"out {o_shape} expected as q {tuple(q.shape)}")
+    if not q.is_cuda or len({t.device for t in (q, k, v, q_offsets, k_offsets, q_lens, k_lens) if t is not None}) != 1:
+        raise ValueError("all tensors of a problem have to be on one GPU")
+    p._device = q.get_device()
     n_seq = q_offsets.numel() - 1
     p.n_q, p.n_k, p.n_seq, p.h_q, p.h_kv, p.d = n_q, n_k, n_seq, h_q, h_kv, d
     p.causal, p.scale = (1 if causal else 0), scale
@@ -281,50 +284,75 @@ def _rows(p, which, name, t):
     """Pointer of a tensor that has to be laid out as the description says."""
     shape, stride = p._of[which]
     st = t.stride()
-    if t.shape == shape and st == stride and t.dtype is torch.bfloat16 and t.is_cuda:
+    if t.shape == shape and st == stride and t.dtype is torch.bfloat16 and t.get_device() == p._device:
         return t.data_ptr()
-    if (t.shape != shape or t.dtype is not torch.bfloat16 or not t.is_cuda or (shape[0] > 1 and st[0] != stride[0]) or
+    if (t.shape != shape or t.dtype is not torch.bfloat16 or t.get_device() != p._device or (shape[0] > 1 and st[0] != stride[0]) or
             (shape[1] > 1 and st[1] != stride[1]) or st[2] != 1):
-        raise ValueError(f"{name}: bf16 {shape} with strides {stride} on the GPU expected, got {t.dtype} {tuple(t.shape)} {st} {t.device}")
+        raise ValueError(f"{name}: bf16 {shape} with strides {stride} on GPU {p._device} expected, got {t.dtype} {tuple(t.shape)} {st} {t.device}")
     return t.data_ptr()
 
 
-def _dense(name, t, shape, dtype):
+def _dense(p, name, t, shape, dtype):
     if t is None:
         return None
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name}: contiguous {dtype} {shape} on the GPU expected, got {t.dtype} {tuple(t.shape)} {t.device}")
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != p._device or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {dtype} {shape} on GPU {p._device} expected, got {t.dtype} {tuple(t.shape)} {t.device}")
     return t.data_ptr()
+
+
+def _scratch(p, t):
+    if t is None:
+        return None, 0
+    if t.get_device() != p._device or not t.is_contiguous():
+        raise ValueError(f"ws: contiguous on GPU {p._device} expected, got {t.device}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _on_device(p, call, *args):
+    """Kernels are launched on the current device: make the problem's device that."""
+    if p._device == (torch.cuda.current_device() if _current_device is None else _current_device()):
+        return call(*args)
+    with torch.cuda.device(p._device):
+        return call(*args)
 
 
 def lsrm_attn_workspace_bytes(p: lsrm_attn_params, which: int) -> int:
     return int(_lib.lsrm_attn_workspace_bytes(ctypes.byref(p), which))
 
 
-def alloc_attn_workspace(p: lsrm_attn_params, which: int, device="cuda"):
-    """Scratch for lsrm_attn_forward (LSRM_WS_FORWARD) or lsrm_attn_backward (LSRM_WS_BACKWARD); None where it needs none."""
+def alloc_attn_workspace(p: lsrm_attn_params, which: int):
+    """Scratch for lsrm_attn_forward (LSRM_WS_FORWARD) or lsrm_attn_backward (LSRM_WS_BACKWARD) on the problem's GPU; None
+    where it needs none.  Calls that may run at the same time need one each."""
     n = lsrm_attn_workspace_bytes(p, which)
-    return torch.empty(n, dtype=torch.uint8, device=device) if n > 0 else None
+    return torch.empty(n, dtype=torch.uint8, device=p._device) if n > 0 else None
 
 
 def lsrm_attn_forward(p, q, k, v, out, lse=None, ws=None, bias=None, stream=None):
     """Dense attention over packed sequences; lse fp32 [n_q, h_q] or None, bias bf16 [h_q, n_buckets] where p has buckets."""
-    nbytes = ws.numel() * ws.element_size() if ws is not None else 0
+    _on_device(p, _attn_forward, p, q, k, v, out, lse, ws, bias, stream)
+
+
+def _attn_forward(p, q, k, v, out, lse, ws, bias, stream):
+    ws_ptr, ws_bytes = _scratch(p, ws)
     _check(_lib.lsrm_attn_forward(ctypes.byref(p), _rows(p, "q", "q", q), _rows(p, "k", "k", k), _rows(p, "v", "v", v),
-                                  _dense("bias", bias, (p.h_q, p.n_buckets), torch.bfloat16), _rows(p, "o", "out", out),
-                                  _dense("lse", lse, (p.n_q, p.h_q), torch.float32), _ptr(ws), nbytes, _stream(stream)),
+                                  _dense(p, "bias", bias, (p.h_q, p.n_buckets), torch.bfloat16), _rows(p, "o", "out", out),
+                                  _dense(p, "lse", lse, (p.n_q, p.h_q), torch.float32), ws_ptr, ws_bytes, _stream(stream)),
            "lsrm_attn_forward")
 
 
 def lsrm_attn_backward(p, q, k, v, out, lse, dout, dq, dk, dv, ws=None, bias=None, dbias=None, stream=None):
     """Gradients of lsrm_attn_forward: dq, dk, dv laid out as q, k, v; dbias as bias, or None."""
-    nbytes = ws.numel() * ws.element_size() if ws is not None else 0
+    _on_device(p, _attn_backward, p, q, k, v, out, lse, dout, dq, dk, dv, ws, bias, dbias, stream)
+
+
+def _attn_backward(p, q, k, v, out, lse, dout, dq, dk, dv, ws, bias, dbias, stream):
+    ws_ptr, ws_bytes = _scratch(p, ws)
     table = (p.h_q, p.n_buckets)
     _check(_lib.lsrm_attn_backward(ctypes.byref(p), _rows(p, "q", "q", q), _rows(p, "k", "k", k), _rows(p, "v", "v", v),
-                                   _dense("bias", bias, table, torch.bfloat16), _rows(p, "o", "out", out),
-                                   _dense("lse", lse, (p.n_q, p.h_q), torch.float32), _rows(p, "o", "dout", dout),
+                                   _dense(p, "bias", bias, table, torch.bfloat16), _rows(p, "o", "out", out),
+                                   _dense(p, "lse", lse, (p.n_q, p.h_q), torch.float32), _rows(p, "o", "dout", dout),
                                    _rows(p, "q", "dq", dq), _rows(p, "k", "dk", dk), _rows(p, "v", "dv", dv),
-                                   _dense("dbias", dbias, table, torch.bfloat16), _ptr(ws), nbytes, _stream(stream)),
+                                   _dense(p, "dbias", dbias, table, torch.bfloat16), ws_ptr, ws_bytes, _stream(stream)),
            "lsrm_attn_backward")
 
 

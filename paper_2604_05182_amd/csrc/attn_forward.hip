@@ -270,7 +270,7 @@ __device__ __forceinline__ bool find_unit(const AttnArgs &a, int x, Sequence &s,
             s.n_k = __builtin_amdgcn_readlane(mine.n_k, at);
             s.k_slot = __builtin_amdgcn_readlane(mine.k_slot, at);
             s.shift = s.n_k - s.n_q;
-            return true;
+            return within >= 0;
         }
         base += __builtin_amdgcn_readlane(upto, 63);
         units += __builtin_amdgcn_readlane(u_upto, 63);

@@ -104,6 +104,103 @@ class Problem:
         return self
 
 
+def all_forward_kernels():
+    """(name, problem): sizes at which a forward call takes each of its ways"""
+    return [
+        ("few", dict(q_lens=[40, 1, 70], h=4, hk=2)),
+        ("few, cut", dict(q_lens=[2, 1, 3], k_lens=[3000, 1025, 2000], h=4, hk=2)),
+        ("many", dict(q_lens=[333, 5, 1030, 128], h=16)),
+        ("many, cut", dict(q_lens=[700, 1500], k_lens=[1400, 2100], h=2, hk=1)),
+    ]
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("way", [0, 1, 2, 3], ids=[name for name, _ in all_forward_kernels()])
+def test_every_way(B, way, bias, causal, d):
+    x = Problem(B, d=d, causal=causal, seed=101, bounds=[-200, -64, -20, -3, 0, 1, 9, 100] if bias else None, **all_forward_kernels()[way][1])
+    x.forward()
+    x.backward()
+    x.check()
+
+
+@pytest.mark.parametrize("way", [0, 1, 2, 3], ids=[name for name, _ in all_forward_kernels()])
+def test_every_way_with_slots(B, way):
+    """rows of slots behind their lengths hold NaN; so do rows before the first and behind the last sequence"""
+    x = Problem(B, d=64, causal=True, slots=133, edge=70, bounds=[-30, -1, 0], seed=102, **all_forward_kernels()[way][1])
+    x.forward()
+    x.backward()
+    x.check()
+
+
+@pytest.mark.parametrize("h", [2, 16])
+def test_more_queries_than_keys(B, h):
+    """causal: the first queries of a sequence see nothing"""
+    x = Problem(B, [600, 900, 130], [100, 899, 1], h=h, d=64, causal=True, seed=103)
+    x.forward()
+    x.backward()
+    x.check()
+
+
+def test_many_rows_of_many_sequences(B):
+    """more sequences than a wavefront has lanes, each of several tiles"""
+    rng = np.random.default_rng(8)
+    x = Problem(B, rng.integers(0, 300, 90), h=8, hk=8, d=32, causal=True, seed=104)
+    x.forward()
+    x.backward()
+    x.check()
+
+
+def test_rows_far_apart(B):
+    """strides at their limit: offsets within a tile pass 2^31 bytes, those of the whole tensor 2^32"""
+    n, step = 150, 1 << 24
+    buf = torch.empty((n - 1) * step + 4 * 64, dtype=torch.bfloat16, device="cuda")
+    x = Problem(B, [n], h=2, d=64, seed=105)
+    for name, head in (("q", 0), ("k", 0), ("v", 2)):
+        far = buf.as_strided((n, 2, 64), (step, 64, 1), head * 64)
+        if name != "q":
+            far.copy_(getattr(x, name))
+            setattr(x, name, far)
+    x.p = B.make_attn_params(x.q, x.k, x.v, int32(x.q_off), int32(x.k_off))
+    x.dk, x.dv = torch.empty_like(buf).as_strided((n, 2, 64), (step, 64, 1)), buf.new_empty(buf.shape).as_strided((n, 2, 64), (step, 64, 1))
+    x.forward()
+    x.backward()
+    x.check()
+
+
+def test_two_at_once(B):
+    """two problems on two streams, workspaces of their own"""
+    xs = [Problem(B, [2000], h=2, d=64, seed=106, causal=True), Problem(B, [1] * 3, [4000, 100, 2500], h=8, hk=1, d=128, seed=107, causal=True)]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    spaces = [(x.workspace(B.LSRM_WS_FORWARD), x.workspace(B.LSRM_WS_BACKWARD)) for x in xs]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for x, st, (wf, wb) in zip(xs, streams, spaces):
+            B.lsrm_attn_forward(x.p, x.q, x.k, x.v, x.out, x.lse, wf, x.bias, st)
+            B.lsrm_attn_backward(x.p, x.q, x.k, x.v, x.out, x.lse, x.dout, x.dq, x.dk, x.dv, wb, stream=st)
+    for x in xs:
+        x.check()
+
+
+def test_offsets_that_do_not_fit(B):
+    """beyond the tensors, descending, lengths past their slots: no access leaves the tensors (what comes out is not specified), and sequences
+    that are described well beside them are right"""
+    q, k, v = rows(100, 4, 64, 1), rows(120, 2, 64, 2), rows(120, 2, 64, 3)
+    for q_off, k_off, q_len, k_len in (([0, 40, 1 << 29], [0, 50, 1 << 30], None, None), ([-7, 40, 30], [60, 50, 120], None, None),
+                                       ([0, 40, 100], [0, 50, 120], [1 << 20, 60], [99, -4]), ([90, 95, 2000], [119, 119, 119], None, None)):
+        for n_seq, causal in ((2, False), (2, True), (70, True)):
+            pad = [0] * (n_seq - 2)
+            args = [int32(list(o) + [o[-1]] * len(pad)) for o in (q_off, k_off)] + [None if l is None else int32(l + pad) for l in (q_len, k_len)]
+            p = B.make_attn_params(q, k, v, *args, causal=causal)
+            out, lse = torch.zeros_like(q), torch.zeros((100, 4), device="cuda")
+            dq, dk, dv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+            B.lsrm_attn_forward(p, q, k, v, out, lse, B.alloc_attn_workspace(p, B.LSRM_WS_FORWARD))
+            B.lsrm_attn_backward(p, q, k, v, out, lse, q, dq, dk, dv, B.alloc_attn_workspace(p, B.LSRM_WS_BACKWARD))
+            torch.cuda.synchronize()
+
+
 LENGTHS = [[1], [2], [31], [32], [33], [64, 1, 65], [127, 128, 129], [0, 5, 0, 70, 0], [200, 3]]
 
 
