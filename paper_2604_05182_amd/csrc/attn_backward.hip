@@ -287,7 +287,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
                 ++g_copy;
             }
         };
-        for (int n = 0; n < RING - 1 && i_copy < i_end; ++n) copy_next();
+        for (int n = 0; n < RING / 2 && i_copy < i_end; ++n) copy_next();
         char *values = lds + kDkvLds<D> + wave * G::TILE + lane * 16;  // of this lane: D / 16 pieces of 16 bytes, 1 KB apart
         // the bias, and of its gradient: sums of the wavefronts' far tiles, sums by distance, skewed tiles
         float *tab = reinterpret_cast<float *>(lds + kDkvLds<D> + kDkvValues<D>), *far = tab + a.group * (a.tab + a.n_buckets) + kMaxBuckets;
@@ -312,16 +312,12 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
         }
         const TileLane<D> t(lane);
         for (int i = i_begin; i < i_end; ++i) {
-            // the tiles behind this one may still be under way (two copy instructions each, with a third of the first wavefront's)
-            constexpr int PER = 2 * G::COPIES / STEP;
-            if (i_copy - i <= 1)
+            // (half the ring's tiles to a barrier, the other half under way)
+            if (((i - i_begin) & (RING / 2 - 1)) == 0) {
                 wait_copies<0>();
-            else if (wave == 0)
-                i_copy - i == 2 ? wait_copies<PER + 1>() : wait_copies<2 * (PER + 1)>();
-            else
-                i_copy - i == 2 ? wait_copies<PER>() : wait_copies<2 * PER>();
-            wg_barrier();
-            if (i_copy < i_end) copy_next();
+                wg_barrier();
+                for (int n = 0; n < RING / 2 && i_copy < i_end; ++n) copy_next();
+            }
             int g_next = g, qt_next = qt + 1;
             if (qt_next == n_t) {
                 qt_next = t0;
