@@ -324,7 +324,7 @@ lsrm_status lsrm_nsa_backward(const lsrm_nsa_params *p, const uint16_t *d_q, con
  * Offsets that do not ascend or leave the tensors, and lengths that do not fit their slot, are cut to what does: no
  * access leaves the tensors, but what such sequences get is unspecified.  q, k, v (and dout) of the sequences have
  * to be finite: a masked key's infinity or NaN may reach the other queries that are worked on beside those that see
- * it.  Rows of no sequence, and rows of a slot behind its length, may hold anything.
+ * it.  Rows of no sequence, and rows of a slot behind its length, may hold anything.  Outputs overlap no input.
  */
 typedef struct lsrm_attn_params {
     int64_t n_q, n_k; /* rows of q (and out) and of k, v, at most 2^30                                     */
@@ -339,8 +339,9 @@ typedef struct lsrm_attn_params {
     const int32_t *d_q_lens;    /* DEVICE, nullable [n_seq]: queries in each slot                         */
     const int32_t *d_k_lens;    /* DEVICE, nullable [n_seq]: keys in each slot; NULL with d_k_offsets NULL: those
                                    of q, as the offsets                                                   */
-    /* {row, head} strides in elements, multiples of 8 up to 2^24 (channels are adjacent); {0, 0}: dense, [rows][heads][d].
-       dout has those of out, dq, dk and dv those of q, k and v: slices of a fused projection work as they are. */
+    /* {row, head} strides in elements, multiples of 8, the rows' up to 2^24, the heads' up to 2^40 (channels are adjacent);
+       {0, 0}: dense, [rows][heads][d].  dout has those of out, dq, dk and dv those of q, k and v: slices of a fused
+       projection and head-major tensors work as they are. */
     int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];
     int32_t n_buckets;            /* 0: no bias; else buckets of the bias, 1 .. 64                         */
     const int32_t *bucket_bounds; /* HOST, read during the call, [n_buckets - 1]: strictly ascending distances at which

@@ -76,7 +76,7 @@ static lsrm_status make_segments(const lsrm_nsa_params *p, const Shape &s, std::
     return LSRM_OK;
 }
 
-// {0, 0} or multiples of 8 that a 32-bit offset within a tile of rows can hold
+// {0, 0} or multiples of 8, the rows' such that a 32-bit offset within a stage of 64 rows can hold it
 static bool strides_of(const int64_t (&given)[2], int heads, int d, int64_t (&out)[2]) {
     if (given[0] == 0 && given[1] == 0) {
         out[0] = (int64_t)heads * d;
@@ -85,9 +85,7 @@ static bool strides_of(const int64_t (&given)[2], int heads, int d, int64_t (&ou
         out[0] = given[0];
         out[1] = given[1];
     }
-    for (int64_t x : out)
-        if (x <= 0 || x % 8 != 0 || x > (int64_t)1 << 24) return false;
-    return true;
+    return out[0] > 0 && out[1] > 0 && out[0] % 8 == 0 && out[1] % 8 == 0 && out[0] <= (int64_t)1 << 24 && out[1] <= (int64_t)1 << 40;
 }
 
 lsrm_status make_attn_args(const lsrm_attn_params *p, AttnArgs *a) {

@@ -45,7 +45,7 @@ def bad_params():
         (params(scale=float("inf")), inv), (params(scale=3e38), inv), (params(d_q_offsets=None), inv), (params(n_k=101), inv),
         (params(n_buckets=-1), inv), (params(n_buckets=2), inv), (params(bounds=[3, 3]), inv), (params(bounds=[3, 1]), inv),
         (params(q_stride=(4, 64)), inv), (params(k_stride=(128, 0)), inv), (params(v_stride=(-128, 64)), inv),
-        (params(o_stride=((1 << 24) + 8, 64)), inv),
+        (params(o_stride=((1 << 24) + 8, 64)), inv), (params(q_stride=(256, (1 << 40) + 8)), inv),
         (params(d=96), uns), (params(n_q=1 << 31, n_k=1 << 31), uns), (params(n_q=1 << 29, n_k=1 << 29, h_q=8), uns),
         (params(n_seq=1 << 24), uns), (params(bounds=list(range(64))), uns), (params(bounds=[0, (1 << 20) + 1]), uns),
         (params(bounds=[-(1 << 20) - 1]), uns), (params(bounds=[0, 1023]), uns), (params(h_q=16, h_kv=1, bounds=[0, 511], n_q=90, n_k=90), uns),

@@ -146,7 +146,20 @@ def test_more_queries_than_keys(B, h):
 def test_many_rows_of_many_sequences(B):
     """more sequences than a wavefront has lanes, each of several tiles"""
     rng = np.random.default_rng(8)
-    x = Problem(B, rng.integers(0, 300, 90), h=8, hk=8, d=32, causal=True, seed=104)
+    x = Problem(B, rng.integers(0, 300, 90), h=8, hk=8, d=32, causal=True, seed=104, slots=11, edge=300)
+    x.forward()
+    x.backward()
+    x.check()
+
+
+@pytest.mark.parametrize("lengths", [[50, 9], [1500, 900]], ids=str)
+def test_head_major(B, lengths):
+    """[heads, rows, channels] underneath"""
+    x = Problem(B, lengths, h=8, hk=4, d=64, causal=True, seed=108)
+    for name in ("q", "k", "v", "out", "dout", "dq", "dk", "dv"):
+        t = getattr(x, name)
+        setattr(x, name, t.transpose(0, 1).contiguous().transpose(0, 1))
+    x.p = B.make_attn_params(x.q, x.k, x.v, int32(x.q_off), causal=True, out=x.out)
     x.forward()
     x.backward()
     x.check()
