@@ -76,7 +76,7 @@ static lsrm_status make_segments(const lsrm_nsa_params *p, const Shape &s, std::
     return LSRM_OK;
 }
 
-// {0, 0} or multiples of 8, the rows' such that a 32-bit offset within a stage of 64 rows can hold it
+// {0, 0} or multiples of 8, the rows' such that a 32-bit offset within a stage of 128 rows can hold it
 static bool strides_of(const int64_t (&given)[2], int heads, int d, int64_t (&out)[2]) {
     if (given[0] == 0 && given[1] == 0) {
         out[0] = (int64_t)heads * d;

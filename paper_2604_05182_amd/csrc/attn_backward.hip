@@ -20,9 +20,10 @@ namespace lsrm {
 
 namespace {
 
-constexpr int kStage = 64;  // keys per stage of the dQ pass
 template <int D>
-constexpr int kDqLds = 2 * kStage * 2 * AttnGeo<D>::ROW;
+constexpr int kStageOf = D == 32 ? 128 : 64;  // keys per stage of the dQ pass
+template <int D>
+constexpr int kDqLds = 2 * kStageOf<D> * 2 * AttnGeo<D>::ROW;
 template <int D>
 constexpr int kDkvSlot = 2 * AttnGeo<D>::TILE + 256;  // 32 rows of q, of dout, and their entries of aux
 // Slots of the dK/dV pass' ring, half of them used between two barriers and half under way: below d = 128 LDS has room for two tiles each.
@@ -34,6 +35,7 @@ constexpr int kDkvLds = 4 * 32 * AttnGeo<D>::OUT_ROW > kDkvRing<D> * kDkvSlot<D>
 template <int D, bool BIAS>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     using G = AttnGeo<D>;
+    constexpr int kStage = kStageOf<D>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv, place = blockIdx.x / a.h_kv;
@@ -104,7 +106,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
         if (st + 1 < st_end) copy_stage(st + 1);
         const char *at = lds + ((st - st_begin) & 1) * (2 * kStage * G::ROW);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kStage / 32; ++h) {
             const int j0 = st * kStage + 32 * h;
             if (j0 >= lim_max) continue;
             const char *kt = at + h * G::TILE, *vt = at + (kStage + 32 * h) * G::ROW;

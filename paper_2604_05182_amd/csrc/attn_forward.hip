@@ -133,18 +133,20 @@ __device__ __forceinline__ void attend(const AttnArgs &a, Rows<D, BIAS> &r, cons
 }
 
 // ---- many rows: four wavefronts of 32 rows share the tiles ------------------------------------------------------------
-// Two stages of 64 keys in LDS, one copied while the other is used, one barrier a stage; two workgroups on a CU at d = 128, four below, which
+// Two stages of 64 keys (128 at d = 32) in LDS, one copied while the other is used, one barrier a stage; two workgroups on a CU at d = 128, four below, which
 // fill each other's waits.  Tried and slower: 64 rows to a wavefront (each tile read from LDS once for both halves; d = 64 263 -> 302 us, at
 // d = 128 one wavefront per SIMD 1042 -> 2388 us); scores of the next tile dealt between the exponentials of this one (d = 64 263 -> 292 us: the
 // registers cost a fourth wavefront); sums by the two-element dot product of the rounded probabilities (d = 64 252 -> 260 us, d = 32 446 -> 430).
-constexpr int kStage = 64;  // keys per stage
 template <int D>
-constexpr int kForwardLds = 2 * kStage * 2 * AttnGeo<D>::ROW;
+constexpr int kStageOf = D == 32 ? 128 : 64;  // keys per stage
+template <int D>
+constexpr int kForwardLds = 2 * kStageOf<D> * 2 * AttnGeo<D>::ROW;
 
 // SPLIT: the keys are cut into a.parts parts, of which sums are left for attn_join_rows.
 template <int D, bool BIAS, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
     using G = AttnGeo<D>;
+    constexpr int kStage = kStageOf<D>;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv, place = blockIdx.x / a.h_kv;
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(256, 2) void attn_forward_kernel(AttnArgs a) {
         wg_barrier();
         if (st + 1 < n_st) copy_stage(st + 1, next);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < kStage / 32; ++h)
             if (st * kStage + 32 * h < r.lim_max)
                 attend<D, BIAS>(a, r, at + h * G::TILE, at + (kStage + 32 * h) * G::ROW, t, st * kStage + 32 * h, hh);
     };
