@@ -229,7 +229,7 @@ def _layout(name, t, heads=None, d=None):
     if c > 1 and t.stride(2) != 1:
         raise ValueError(f"{name}: channels have to be adjacent")
     head = t.stride(1) if h > 1 else c
-    row = t.stride(0) if rows > 1 else h * head
+    row = t.stride(0) if rows > 1 else h * c  # (not heads times their stride: those of one row of a large cache may be far apart)
     if row <= 0 or head <= 0:
         raise ValueError(f"{name}: expanded rows or heads are not taken, strides {t.stride()}")
     return tuple(t.shape), (row, head)

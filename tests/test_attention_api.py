@@ -217,3 +217,12 @@ def test_bounds_let_rounding_pass_and_mistakes_fail():
         for name in ("out", "dq", "dk", "dv") + (() if "scale" in wrong else ("dbias",)):  # (dbias hardly goes by the scale)
             with pytest.raises(AssertionError):
                 R.check(name, bad[name], val[name], err[name])
+
+
+def test_one_row_of_a_large_cache():
+    """The heads of a single row may lie as far apart as the format allows: the row's own stride says nothing."""
+    cache = torch.empty((8, 70000, 128), dtype=torch.bfloat16, device="meta").transpose(0, 1)
+    assert B._layout("k", cache) == ((70000, 8, 128), (128, 70000 * 128))
+    shape, stride = B._layout("k", cache[:1])
+    assert shape == (1, 8, 128) and stride == (8 * 128, 70000 * 128)
+    assert B._layout("k", cache[:, :1]) == ((70000, 1, 128), (128, 128))

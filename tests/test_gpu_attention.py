@@ -508,3 +508,17 @@ def test_beside_the_sparse_layer(B):
     q, k, v = (t.float().cpu().numpy() for t in (x.q, x.k, x.out))
     ref = oracle.nsa_forward(q, k, v, oracle.pool(k), oracle.pool(v), idx.cpu().numpy(), gates, cfg.seg_offsets(), cfg.window)
     assert np.abs(out.float().cpu().numpy() - ref).max() <= 2e-2
+
+
+def test_one_row_of_a_large_cache(B):
+    """One key in a head-major cache whose heads lie 2^23 elements apart"""
+    n, h, d = 1 << 16, 4, 128
+    cache = torch.full((2, h, n, d), float("nan"), dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+    k, v = cache[0, :1], cache[1, :1]
+    k.copy_(rows(1, h, d, 1))
+    v.copy_(rows(1, h, d, 2))
+    q = rows(1, h, d, 3)
+    out = torch.empty_like(q)
+    p = B.make_attn_params(q, k, v, int32([0, 1]), int32([0, 1]), causal=True)
+    B.lsrm_attn_forward(p, q, k, v, out, None, B.alloc_attn_workspace(p, B.LSRM_WS_FORWARD))
+    assert torch.equal(out, v)  # one key: its probability is one
