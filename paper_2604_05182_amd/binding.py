@@ -7,6 +7,7 @@ is no CPU fallback: if the library has not been built, importing this module rai
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 
 import torch
@@ -243,6 +244,13 @@ def _int32(name, t, n):
     return t.data_ptr()
 
 
+def _bounds(bucket_bounds):
+    bounds = [operator.index(x) for x in bucket_bounds]
+    if any(not -(1 << 31) <= x < 1 << 31 for x in bounds):  # (ctypes would cut them to 32 bits)
+        raise ValueError("bucket_bounds: 32-bit integers expected")
+    return (ctypes.c_int32 * max(len(bounds), 1))(*bounds)
+
+
 def make_attn_params(q, k, v, q_offsets, k_offsets=None, q_lens=None, k_lens=None, causal=False, scale=0.0,
                      bucket_bounds=None, out=None) -> lsrm_attn_params:
     """Describes a problem by its tensors: q bf16 [n_q, h_q, d], k, v bf16 [n_k, h_kv, d] (views of a projection are fine:
@@ -273,7 +281,7 @@ def make_attn_params(q, k, v, q_offsets, k_offsets=None, q_lens=None, k_lens=Non
     p._of = {"q": ((n_q, h_q, d), q_st + (1,)), "k": ((n_k, h_kv, d), k_st + (1,)), "v": ((n_k, h_kv, d), v_st + (1,)),
              "o": ((n_q, h_q, d), o_st + (1,))}
     if bucket_bounds is not None:
-        arr = (ctypes.c_int32 * max(len(bucket_bounds), 1))(*[int(x) for x in bucket_bounds])
+        arr = _bounds(bucket_bounds)
         p._bounds = arr
         p.n_buckets = len(bucket_bounds) + 1
         p.bucket_bounds = ctypes.cast(arr, ctypes.POINTER(ctypes.c_int32))

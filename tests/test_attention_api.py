@@ -226,3 +226,10 @@ def test_one_row_of_a_large_cache():
     shape, stride = B._layout("k", cache[:1])
     assert shape == (1, 8, 128) and stride == (8 * 128, 70000 * 128)
     assert B._layout("k", cache[:, :1]) == ((70000, 1, 128), (128, 128))
+
+
+@pytest.mark.parametrize("bounds, error", [([-3, 0, 1 << 32], ValueError), ([-(1 << 31) - 1, 0], ValueError), ([-3, 0.5], TypeError)])
+def test_bounds_are_not_cut_to_fit(bounds, error):
+    with pytest.raises(error):
+        B._bounds(bounds)
+    assert list(B._bounds([np.int64(-3), torch.tensor(4)])) == [-3, 4]
