@@ -364,6 +364,7 @@ __global__ __launch_bounds__((64 * kFewWaves<D, SPLIT || BIAS>), 1) void attn_fe
     }
     for (int slot = 0; j0 < j_end; j0 += STEP, slot ^= 1) {
         if (j0 + STEP < j_end) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // nobody waits for this slot's last reads but this wavefront
             copy_tile(j0 + STEP, slot ^ 1);
             wait_copies<2 * G::COPIES>();
         } else {
