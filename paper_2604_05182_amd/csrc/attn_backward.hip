@@ -5,7 +5,7 @@
 // Two passes that each own their output rows (no atomics between workgroups, one order of sums):
 //   attn_dq_kernel   128 query rows to a workgroup, one query row per lane (S^T = K Q^T), walks the keys; works out D for itself
 //                    and leaves it, with the log-sum-exp, for the other pass.
-//   attn_dkv_kernel  128 keys of a key/value head to a workgroup, one key per lane (S = Q K^T), walks the queries of the heads that
+//   attn_dkv_kernel  128 keys of a key/value head to a workgroup (32 in small problems), one key per lane (S = Q K^T), walks the queries of the heads that
 //                    read them; sums dS by distance.
 // Seven contractions where five are needed: the price of gradients that are the same in every run (one pass would have to add dQ from many
 // workgroups).  P and dS are rounded to bf16, to nearest, as operands; D comes from the rounded outputs, which makes dQ's error 1.5 of that
@@ -238,26 +238,61 @@ constexpr int kSkew = D == 128 ? 4 : 16;
 template <int D>
 constexpr int kDkvValues = D == 128 ? 4 * AttnGeo<D>::TILE : 0;
 
-template <int D, bool BIAS>
-__global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
+// FEW: where workgroups of 128 keys leave most of the chip empty, 32 keys to a workgroup: its four wavefronts hold the same keys, walk every fourth
+// tile of queries each, through a ring of two slots of their own and with no barrier, and their sums meet in LDS once, at the end.  The longest
+// walk, which is what small problems take, is a quarter as long, with nothing left to a launch behind.  (7 sequences of up to 257
+// tokens, 8 heads of 32 on 4, bias: training step 53.6 -> 39.4 us; backward of 4 x 512 tokens, causal, 8 heads of 64 on 4: 41.8 -> 25.0 us.)
+template <int D>
+constexpr int kFewPitch = D + 4;  // floats of a row where the sums meet
+template <int D>
+constexpr int kFewRing = 2 * kDkvSlot<D> > 2 * 32 * kFewPitch<D> * 4 ? 2 * kDkvSlot<D> : 2 * 32 * kFewPitch<D> * 4;  // per wavefront
+
+// What a wavefront has summed of the bias' gradient of one query head is added up by buckets into dst (LDS), and the sums begin anew.
+__device__ __forceinline__ void flush_bias_wave(const AttnArgs &a, const int *bounds, float *near, float lo, float hi, float *dst, int lane) {
+    for (int x = 32; x > 0; x /= 2) {
+        lo += __shfl_xor(lo, x);
+        hi += __shfl_xor(hi, x);
+    }
+    asm volatile("" ::: "memory");  // (lanes read what others wrote, in order)
+    const int n = a.n_buckets;
+    for (int b = lane / 4; b < (n + 15) / 16 * 16; b += 16) {  // four lanes to a bucket
+        float sum = 0.f;
+        if (b < n) {
+            const int from = b > 0 ? bias_entry(a, bounds[b - 1]) : 0, to = b < n - 1 ? bias_entry(a, bounds[b]) : a.tab;
+            for (int x = from + lane % 4; x < to; x += 4) sum += near[x];
+        }
+        sum += __shfl_xor(sum, 1);
+        sum += __shfl_xor(sum, 2);
+        if (b == 0) sum += lo;
+        if (b == n - 1) sum += hi;
+        if (b < n && lane % 4 == 0) dst[b] = sum;
+    }
+    asm volatile("" ::: "memory");
+    for (int x = lane; x < a.tab; x += 64) near[x] = 0.f;
+    asm volatile("" ::: "memory");
+}
+
+template <int D, bool BIAS, bool FEW>
+__global__ __launch_bounds__(256, FEW && D == 128 ? 1 : 2) void attn_dkv_kernel(AttnArgs a) {
     using G = AttnGeo<D>;
-    constexpr bool V_LDS = kDkvValues<D> > 0;
+    constexpr bool V_LDS = !FEW && kDkvValues<D> > 0;
+    constexpr int KEYS = FEW ? 32 : 128;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv, place = blockIdx.x / a.h_kv;
-    const int part = place % a.parts;
+    const int part = FEW ? 0 : place % a.parts;
     int tile = 0, seq;
     Sequence s = {};
-    const bool none = !find_tile<true>(a, 1, 128, place / a.parts, s, tile, seq);
-    const int j_wg = tile * 128;
-    const int j0 = j_wg + wave * 32, j = j0 + (lane & 31);
+    const bool none = !find_tile<true>(a, 1, KEYS, FEW ? place : place / a.parts, s, tile, seq);
+    const int j_wg = tile * KEYS;
+    const int j0 = j_wg + (FEW ? 0 : wave * 32), j = j0 + (lane & 31);
     const bool live = j < s.n_k;
     // query tiles of 32: those of a head from the first that sees a key of this workgroup on, head after head
     const int n_t = (s.n_q + 31) / 32, t0 = a.causal ? min(max(j_wg - s.shift, 0) / 32, n_t) : 0;
-    const int n_all = !none && j_wg < s.n_k ? a.group * (n_t - t0) : 0, per = uniform((n_all + a.parts - 1) / a.parts);
+    const int n_all = !none && j_wg < s.n_k ? a.group * (n_t - t0) : 0, per = FEW ? n_all : uniform((n_all + a.parts - 1) / a.parts);
     const int i_begin = part * per, i_end = min(i_begin + per, n_all);
     float *sums = BIAS && a.part_bias != nullptr ? a.part_bias + ((int64_t)place * a.h_q + head_kv * a.group) * a.n_buckets : nullptr;
-    if (BIAS && sums != nullptr) {  // heads that this part does not walk
+    if (BIAS && sums != nullptr && (!FEW || none)) {  // heads that this part does not walk
         const int g_first = i_begin < i_end ? i_begin / (n_t - t0) : a.group, g_last = i_begin < i_end ? (i_end - 1) / (n_t - t0) : -1;
         for (int i = threadIdx.x; i < a.group * a.n_buckets; i += 256) {
             const int g = i / a.n_buckets;
@@ -265,6 +300,17 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
         }
     }
     if (none) return;
+    // in LDS behind the tiles: the bias; of its gradient: sums of the wavefronts' far tiles, sums by distance, skewed tiles (FEW: sums by distance,
+    // skewed tiles, sums by head and bucket)
+    char *ring = lds + (FEW ? wave * kFewRing<D> : 0);
+    float *tab = reinterpret_cast<float *>(lds + (FEW ? 4 * kFewRing<D> : kDkvLds<D> + kDkvValues<D>));
+    float *far = tab + a.group * (a.tab + a.n_buckets) + kMaxBuckets, *near = FEW ? far : far + 8;
+    float *skew = near + 4 * a.tab + wave * (Skew<kSkew<D>>::BYTES / 4), *by_bucket = near + 4 * a.tab + Skew<kSkew<D>>::BYTES;
+    if (FEW && BIAS && sums != nullptr) {  // (each wavefront its own)
+        for (int x = lane; x < a.tab; x += 64) near[wave * a.tab + x] = 0.f;
+        for (int x = lane; x < Skew<kSkew<D>>::BYTES / 4; x += 64) skew[x] = 0.f;
+        for (int x = lane; x < a.group * a.n_buckets; x += 64) by_bucket[wave * a.group * a.n_buckets + x] = 0.f;
+    }
     bf16x8 kf[G::NS], vf[V_LDS ? 1 : G::NS];
     f32x16 dk[G::ND], dv[G::ND];
 #pragma unroll
@@ -274,36 +320,40 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
     if (i_begin < i_end) {
         const uint32_t q_row = (uint32_t)a.qs[0] * 2, o_row = (uint32_t)a.os[0] * 2;
         const CopyLane<D> c(lane);
-        constexpr int STEP = G::COPIES < 4 ? G::COPIES : 4, RING = kDkvRing<D>;
+        constexpr int STEP = FEW ? 1 : G::COPIES < 4 ? G::COPIES : 4, RING = FEW ? 2 : kDkvRing<D>, STRIDE = FEW ? 4 : 1;
+        // tile i of the walk goes to slot (i - i_begin) / STRIDE of the ring
         auto copy_tile = [&](int i, int g, int qt) {
-            char *at = lds + ((i - i_begin) & (RING - 1)) * kDkvSlot<D>;
+            char *at = ring + ((i - i_begin) / STRIDE & (RING - 1)) * kDkvSlot<D>;
             const int head = head_kv * a.group + g, avail = s.n_q - 32 * qt;
             const int64_t row = s.q0 + 32 * qt;
             copy_rows<D, 32, STEP>(reinterpret_cast<const char *>(a.q + row * a.qs[0] + head * a.qs[1]), q_row, avail, at, wave % STEP, c);
             copy_rows<D, 32, STEP>(reinterpret_cast<const char *>(a.dout + row * a.os[0] + head * a.os[1]), o_row, avail, at + G::TILE,
                                    wave % STEP, c);
-            if (wave == 0)
+            if (FEW || wave == 0)
                 copy_256_to_lds(a.aux + (int64_t)head * a.n_q + row, min(lane & 31, avail - 1) * 8 + hh * 4, at + 2 * G::TILE);
         };
-        int g = uniform(i_begin / (n_t - t0)), qt = t0 + uniform(i_begin % (n_t - t0)), g_copy = g, qt_copy = qt, i_copy = i_begin;
+        const int i_first = i_begin + (FEW ? wave : 0);
+        int g = uniform(i_first / (n_t - t0)), qt = t0 + uniform(i_first % (n_t - t0)), g_copy = g, qt_copy = qt, i_copy = i_first;
         auto copy_next = [&] {
             copy_tile(i_copy, g_copy, qt_copy);
-            ++i_copy;
-            if (++qt_copy == n_t) {
+            i_copy += STRIDE;
+            qt_copy += STRIDE;
+            if constexpr (FEW) {
+                while (qt_copy >= n_t) {
+                    qt_copy -= n_t - t0;
+                    ++g_copy;
+                }
+            } else if (qt_copy == n_t) {
                 qt_copy = t0;
                 ++g_copy;
             }
         };
         for (int n = 0; n < RING / 2 && i_copy < i_end; ++n) copy_next();
         char *values = lds + kDkvLds<D> + wave * G::TILE + lane * 16;  // of this lane: D / 16 pieces of 16 bytes, 1 KB apart
-        // the bias, and of its gradient: sums of the wavefronts' far tiles, sums by distance, skewed tiles
-        float *tab = reinterpret_cast<float *>(lds + kDkvLds<D> + kDkvValues<D>), *far = tab + a.group * (a.tab + a.n_buckets) + kMaxBuckets;
-        float *near = far + 8;
-        float *skew = near + 4 * a.tab + wave * (Skew<kSkew<D>>::BYTES / 4);
         float lo = 0.f, hi = 0.f;
         if (BIAS) {
             expand_bias(a, head_kv, tab, 256);
-            if (sums != nullptr)
+            if (!FEW && sums != nullptr)
                 for (int i = threadIdx.x; i < 4 * a.tab + Skew<kSkew<D>>::BYTES; i += 256) near[i] = 0.f;  // (and the four wavefronts' skews)
         }
         const int jc = min(j, s.n_k - 1);
@@ -318,21 +368,38 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
                 vf[ks] = *reinterpret_cast<const bf16x8 *>(vp + 16 * ks);
         }
         const TileLane<D> t(lane);
-        for (int i = i_begin; i < i_end; ++i) {
-            // (half the ring's tiles to a barrier, the other half under way)
-            if (((i - i_begin) & (RING / 2 - 1)) == 0) {
+        if (FEW && BIAS) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            wg_barrier();
+        }
+        for (int i = i_first; i < i_end; i += STRIDE) {
+            if constexpr (FEW) {
+                if (i_copy < i_end) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // nobody waits for this slot's last reads but this wavefront
+                    copy_next();
+                    wait_copies<2 * G::COPIES + 1>();
+                } else {
+                    wait_copies<0>();
+                }
+            } else if (((i - i_begin) & (RING / 2 - 1)) == 0) {
+                // (half the ring's tiles to a barrier, the other half under way)
                 wait_copies<0>();
                 wg_barrier();
                 for (int n = 0; n < RING / 2 && i_copy < i_end; ++n) copy_next();
             }
-            int g_next = g, qt_next = qt + 1;
-            if (qt_next == n_t) {
+            int g_next = g, qt_next = qt + STRIDE;
+            if constexpr (FEW) {
+                while (qt_next >= n_t) {
+                    qt_next -= n_t - t0;
+                    ++g_next;
+                }
+            } else if (qt_next == n_t) {
                 qt_next = t0;
                 ++g_next;
             }
             const int p0 = 32 * qt + s.shift;  // position of the tile's first query
             if (j0 < s.n_k && !(a.causal && p0 + 31 < j0)) {
-                const char *at = lds + ((i - i_begin) & (RING - 1)) * kDkvSlot<D>;
+                const char *at = ring + ((i - i_begin) / STRIDE & (RING - 1)) * kDkvSlot<D>;
                 const float *aux = reinterpret_cast<const float *>(at + 2 * G::TILE) + 8 * hh;
                 f32x16 p = mfma_rows<D>(splat(0.f), at, t, kf), dp;
                 const bool behind = BIAS && j0 + 31 - p0 < a.b0, ahead = BIAS && j0 - p0 - 31 >= a.b_last;
@@ -445,8 +512,12 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
                 to_b_operand(dp, b);
                 mfma_transposed<D>(dk, at, t, b);
             }
-            if (BIAS && sums != nullptr && (g_next != g || i + 1 == i_end)) {
-                flush_bias(a, near, far, lo, hi, sums + g * a.n_buckets);
+            if (BIAS && sums != nullptr && (g_next != g || i + STRIDE >= i_end)) {
+                if constexpr (FEW)
+                    flush_bias_wave(a, reinterpret_cast<const int *>(tab + a.group * a.tab), near + wave * a.tab, lo, hi,
+                                    by_bucket + (wave * a.group + g) * a.n_buckets, lane);
+                else
+                    flush_bias(a, near, far, lo, hi, sums + g * a.n_buckets);
                 lo = hi = 0.f;
             }
             g = g_next;
@@ -454,8 +525,44 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnArgs a) {
         }
     }
     wait_copies<0>();
-    wg_barrier();
+    if (!FEW) wg_barrier();
     mfma_settle();
+    if constexpr (FEW) {
+        // the wavefronts' sums meet
+        float *mine = reinterpret_cast<float *>(ring) + (lane & 31) * kFewPitch<D> + 4 * hh;
+#pragma unroll
+        for (int dt = 0; dt < G::ND; ++dt)
+#pragma unroll
+            for (int gq = 0; gq < 4; ++gq) {
+                *reinterpret_cast<f32x4 *>(mine + 32 * dt + 8 * gq) = f32x4{dk[dt][4 * gq], dk[dt][4 * gq + 1], dk[dt][4 * gq + 2], dk[dt][4 * gq + 3]};
+                *reinterpret_cast<f32x4 *>(mine + 32 * kFewPitch<D> + 32 * dt + 8 * gq) =
+                    f32x4{dv[dt][4 * gq], dv[dt][4 * gq + 1], dv[dt][4 * gq + 2], dv[dt][4 * gq + 3]};
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wg_barrier();
+        if (BIAS && sums != nullptr) {
+            const int n = a.group * a.n_buckets;
+            for (int i = threadIdx.x; i < n; i += 256) sums[i] = (by_bucket[i] + by_bucket[n + i]) + (by_bucket[2 * n + i] + by_bucket[3 * n + i]);
+        }
+        const int row = threadIdx.x / 8, c0 = 4 * (threadIdx.x % 8);
+        if (j0 + row >= s.k_slot) return;
+        const bool live = j0 + row < s.n_k;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const float mul = which == 0 ? a.scale : 1.0f;
+            uint16_t *dst = (which == 0 ? a.dk + (s.k0 + j0 + row) * a.ks[0] + head_kv * a.ks[1] : a.dv + (s.k0 + j0 + row) * a.vs[0] + head_kv * a.vs[1]) + c0;
+#pragma unroll
+            for (int ch = 0; ch < D; ch += 32) {
+                f32x4 x[4];
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    x[w] = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(lds + w * kFewRing<D>) + (which * 32 + row) * kFewPitch<D> + c0 + ch);
+                const f32x4 y = ((x[0] + x[1]) + (x[2] + x[3])) * mul;
+                *reinterpret_cast<uint2 *>(dst + ch) = live ? make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])) : make_uint2(0, 0);
+            }
+        }
+        return;
+    }
     if (a.parts == 1) {
         // (a key/value head's rows: the same as query rows of a group of one)
         char *stage = lds + wave * 32 * G::OUT_ROW;
@@ -547,8 +654,14 @@ __global__ __launch_bounds__(1024) void attn_sum_bias(AttnArgs a) {
     }
 }
 
+// bytes of LDS of a workgroup of the dK/dV pass' few keys
+template <int D>
+int64_t few_lds(const AttnArgs &a) {
+    return 4 * kFewRing<D> + (a.n_buckets > 0 ? (bias_lds_floats(a) + 4 * (int64_t)a.tab + Skew<kSkew<D>>::BYTES + 4 * a.group * a.n_buckets) * 4 : 0);
+}
 struct WsLayout {
     int q_slots, k_slots, q_parts, k_parts;
+    bool few_keys;
     size_t aux, part_q, part_k, part_v, part_bias, total;
 };
 WsLayout layout(const AttnArgs &a, int d) {
@@ -559,8 +672,22 @@ WsLayout layout(const AttnArgs &a, int d) {
     const double steps = walk_steps(a), full = full_chip(d);
     w.q_parts = best_parts(steps, d == 32 ? 450 : d == 64 ? 600 : 1050, ((double)rows / 128 + 1) * a.h_kv, full, (double)a.n_q * a.h_q * d * 8,
                            (int64_t)a.n_k / a.n_seq / 32, (int64_t)w.q_slots * a.h_kv);
-    w.k_parts = best_parts(steps, d == 32 ? 600 : d == 64 ? 800 : 1400, ((double)a.n_k / 128 + 1) * a.h_kv, full, (double)a.n_k * a.h_kv * d * 16,
-                           rows / a.n_seq / 32, (int64_t)w.k_slots * a.h_kv);
+    const double k_cycles = d == 32 ? 600 : d == 64 ? 800 : 1400, k_wgs = ((double)a.n_k / 128 + 1) * a.h_kv;
+    const int64_t walk = rows / a.n_seq / 32, slots32 = a.n_k / 32 + a.n_seq;
+    double cut, few;
+    w.k_parts = best_parts(steps, k_cycles, k_wgs, full, (double)a.n_k * a.h_kv * d * 16, walk, (int64_t)w.k_slots * a.h_kv, &cut);
+    // 32 keys to a workgroup: where those are all on the chip at the same time, and cutting the walks of 128 does not promise more.  Neither takes less
+    // than the steps behind each other in its longest walks, at about twice the cycles of a step on a full chip.
+    best_parts(steps, k_cycles, 4 * k_wgs, full, 0, 0, 0, &few);
+    const double chain = walk * k_cycles * 2 / 2.1e3;
+    few = std::max(few, chain / 4);
+    cut = std::max(cut, chain / w.k_parts + (w.k_parts > 1 ? 4 : 0));
+    const int64_t lds = d == 32 ? few_lds<32>(a) : d == 64 ? few_lds<64>(a) : few_lds<128>(a);
+    w.few_keys = slots32 * a.h_kv <= (d == 128 ? 256 : 512) && lds <= 160 * 1024 && few <= cut;
+    if (w.few_keys) {
+        w.k_slots = (int)slots32;
+        w.k_parts = 1;
+    }
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -594,8 +721,11 @@ lsrm_status launch_backward_d(AttnArgs a, void *ws, hipStream_t st) {
         if (rc != LSRM_OK) return rc;
         if (w.q_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, true>, ((int64_t)a.n_q / (2048 / D) + a.n_seq) * a.h_q, 256, 0, a, st)) != LSRM_OK) return rc;
         a.parts = w.k_parts;
-        rc = launch_attn(bias ? &attn_dkv_kernel<D, true> : &attn_dkv_kernel<D, false>, (int64_t)w.k_slots * a.h_kv * w.k_parts, 256,
-                         kDkvLds<D> + kDkvValues<D> + (bias ? n_tab + 32 + (a.dbias != nullptr ? 16 * a.tab + 4 * Skew<kSkew<D>>::BYTES : 0) : 0), a, st);
+        if (w.few_keys)
+            rc = launch_attn(bias ? &attn_dkv_kernel<D, true, true> : &attn_dkv_kernel<D, false, true>, (int64_t)w.k_slots * a.h_kv, 256, (int)few_lds<D>(a), a, st);
+        else
+            rc = launch_attn(bias ? &attn_dkv_kernel<D, true, false> : &attn_dkv_kernel<D, false, false>, (int64_t)w.k_slots * a.h_kv * w.k_parts, 256,
+                             kDkvLds<D> + kDkvValues<D> + (bias ? n_tab + 32 + (a.dbias != nullptr ? 16 * a.tab + 4 * Skew<kSkew<D>>::BYTES : 0) : 0), a, st);
         if (rc != LSRM_OK) return rc;
         a.n_slots = w.k_slots * w.k_parts;  // (of the bias' sums)
         if (w.k_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, false>, ((int64_t)a.n_k / (2048 / D) + a.n_seq) * a.h_kv * 2, 256, 0, a, st)) != LSRM_OK) return rc;

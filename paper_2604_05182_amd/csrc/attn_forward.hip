@@ -566,7 +566,7 @@ lsrm_status launch_forward_d(AttnArgs a, void *ws, hipStream_t st) {
 
 }  // namespace
 
-int best_parts(double steps, double cycles, double workgroups, double full, double bytes, int64_t walk, int64_t grid) {
+int best_parts(double steps, double cycles, double workgroups, double full, double bytes, int64_t walk, int64_t grid, double *time) {
     const double work = steps * cycles / 4 / 256 / 2.1e3;  // us, with the chip full
     int best = 1;
     double least = 0;
@@ -577,6 +577,7 @@ int best_parts(double steps, double cycles, double workgroups, double full, doub
             least = t;
         }
     }
+    if (time != nullptr) *time = least;
     return best;
 }
 

@@ -327,8 +327,8 @@ __device__ __forceinline__ void store_query_rows(const AttnArgs &a, const Sequen
 // full from `full` workgroups on; 3.5 bytes of sums a nanosecond, and 4 us for the launch):
 //   T(parts) = steps / min(1, workgroups parts / full) + (parts > 1) (4 us + parts bytes / 3.5 TB/s)
 // Always 512 workgroups instead: 32 heads of 32 on 2, 6372 tokens 450 -> 390 us a training step.
-// walk: steps of an average walk (a part has four at least); grid: workgroups that are launched for each part.
-int best_parts(double steps, double cycles, double workgroups, double full, double bytes, int64_t walk, int64_t grid);
+// walk: steps of an average walk (a part has four at least); grid: workgroups that are launched for each part; time: T, in us.
+int best_parts(double steps, double cycles, double workgroups, double full, double bytes, int64_t walk, int64_t grid, double *time = nullptr);
 // walk steps of single wavefronts (32 x 32): those of average sequences, half of them where causal
 inline double walk_steps(const AttnArgs &a) {
     return (double)a.n_q * a.group * a.h_kv / 32 * a.n_k / a.n_seq / 32 * (a.causal && a.n_q == a.n_k ? 0.5 : 1.0);

@@ -522,3 +522,19 @@ def test_one_row_of_a_large_cache(B):
     p = B.make_attn_params(q, k, v, int32([0, 1]), int32([0, 1]), causal=True)
     B.lsrm_attn_forward(p, q, k, v, out, None, B.alloc_attn_workspace(p, B.LSRM_WS_FORWARD))
     assert torch.equal(out, v)  # one key: its probability is one
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("case", [
+    dict(q_lens=[257, 100, 30, 1, 180], h=8, hk=4),               # few keys to a workgroup
+    dict(q_lens=[1, 40, 0, 5], k_lens=[33, 0, 64, 200], h=6, hk=1),  # the same; fewer tiles of queries than wavefronts, none at all
+    dict(q_lens=[300, 260], h=32),                                # many
+    dict(q_lens=[2048], h=8, hk=2),                               # many, walks cut
+], ids=["few", "few, short", "many", "many, cut"])
+def test_every_way_backward(B, case, bias, causal, d):
+    x = Problem(B, d=d, causal=causal, seed=103, slots=9, edge=3, bounds=[-90, -17, -1, 0, 1, 40] if bias else None, **case)
+    x.forward()
+    x.backward()
+    x.check()
