@@ -3,7 +3,7 @@
 // With P = softmax probabilities recomputed from the saved log-sum-exp, D_i = dout_i . out_i, dP = dout V^T:
 //     dV = P^T dout      dS = P o (dP - D)      dQ = scale dS K      dK = scale dS^T Q      dB[b] = sum of dS over bucket b
 // Two passes that each own their output rows (no atomics between workgroups, one order of sums):
-//   attn_dq_kernel   128 query rows to a workgroup, one query row per lane (S^T = K Q^T), walks the keys; works out D for itself
+//   attn_dq_kernel   128 query rows to a workgroup (32 in small problems), one query row per lane (S^T = K Q^T), walks the keys; works out D for itself
 //                    and leaves it, with the log-sum-exp, for the other pass.
 //   attn_dkv_kernel  128 keys of a key/value head to a workgroup (32 in small problems), one key per lane (S = Q K^T), walks the queries of the heads that
 //                    read them; sums dS by distance.
@@ -24,6 +24,12 @@ template <int D>
 constexpr int kStageOf = D == 32 ? 128 : 64;  // keys per stage of the dQ pass
 template <int D>
 constexpr int kDqLds = 2 * kStageOf<D> * 2 * AttnGeo<D>::ROW;
+// FEW: the wavefronts take turns at the keys of the same 32 rows, each through a ring of two tiles of its own, and meet in LDS at the end.
+// (Backward of 5 sequences of up to 257 tokens, 8 heads on 4: d = 32 14.9 -> 12.7 us, d = 64 18.6 -> 15.5, d = 128 29.7 -> 25.5.)
+template <int D>
+constexpr int kDqFewRing = 2 * 2 * AttnGeo<D>::TILE > 32 * (D + 4) * 4 ? 2 * 2 * AttnGeo<D>::TILE : 32 * (D + 4) * 4;
+template <int D>
+constexpr int kDqFewLds = 4 * (kDqFewRing<D> + 128);
 template <int D>
 constexpr int kDkvSlot = 2 * AttnGeo<D>::TILE + 256;  // 32 rows of q, of dout, and their entries of aux
 // Slots of the dK/dV pass' ring, half of them used between two barriers and half under way: below d = 128 LDS has room for two tiles each.
@@ -32,39 +38,44 @@ constexpr int kDkvRing = D == 128 ? 2 : 4;
 template <int D>
 constexpr int kDkvLds = 4 * 32 * AttnGeo<D>::OUT_ROW > kDkvRing<D> * kDkvSlot<D> ? 4 * 32 * AttnGeo<D>::OUT_ROW : kDkvRing<D> * kDkvSlot<D>;
 
-template <int D, bool BIAS>
+template <int D, bool BIAS, bool FEW>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     using G = AttnGeo<D>;
-    constexpr int kStage = kStageOf<D>;
+    constexpr int kStage = FEW ? 32 : kStageOf<D>, ROWS = FEW ? 32 : 128, STRIDE = FEW ? 4 : 1;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5;
     const int head_kv = blockIdx.x % a.h_kv, place = blockIdx.x / a.h_kv;
-    const int part = place % a.parts;
+    const int part = FEW ? 0 : place % a.parts;
     int tile, seq;
     Sequence s;
-    if (!find_tile<false>(a, a.group, 128, place / a.parts, s, tile, seq)) return;
+    if (!find_tile<false>(a, a.group, ROWS, FEW ? place : place / a.parts, s, tile, seq)) return;
     const int slot_rows = s.q_slot * a.group, n_rows = s.n_q * a.group;
-    if (a.causal) tile = (slot_rows - 1) / 128 - tile;  // the last rows, which see most keys, first
-    const int v_wg = tile * 128;
+    if (a.causal) tile = (slot_rows - 1) / ROWS - tile;  // the last rows, which see most keys, first
+    const int v_wg = tile * ROWS;
     auto seen = [&](int pos) { return a.causal ? min(max(pos + 1, 0), s.n_k) : s.n_k; };
-    const int keys = v_wg < n_rows ? seen(uniform((unsigned)min(v_wg + 127, n_rows - 1) / (unsigned)a.group) + s.shift) : 0;
-    const int st_all = (keys + kStage - 1) / kStage, st_per = uniform((st_all + a.parts - 1) / a.parts);
-    const int st_begin = part * st_per, st_end = min(st_begin + st_per, st_all);
+    const int keys = v_wg < n_rows ? seen(uniform((unsigned)min(v_wg + ROWS - 1, n_rows - 1) / (unsigned)a.group) + s.shift) : 0;
+    const int st_all = (keys + kStage - 1) / kStage, st_per = FEW ? st_all : uniform((st_all + a.parts - 1) / a.parts);
+    const int st_begin = part * st_per + (FEW ? wave : 0), st_end = FEW ? st_all : min(st_begin + st_per, st_all);
     const char *kb = reinterpret_cast<const char *>(a.k + s.k0 * a.ks[0] + head_kv * a.ks[1]);
     const char *vb = reinterpret_cast<const char *>(a.v + s.k0 * a.vs[0] + head_kv * a.vs[1]);
     const uint32_t k_row = (uint32_t)a.ks[0] * 2, v_row = (uint32_t)a.vs[0] * 2;
     const CopyLane<D> c(lane);
+    char *ring = lds + (FEW ? wave * kDqFewRing<D> : 0);
     auto copy_stage = [&](int st) {
-        char *at = lds + ((st - st_begin) & 1) * (2 * kStage * G::ROW);
+        char *at = ring + ((st - st_begin) / STRIDE & 1) * (2 * kStage * G::ROW);
         const int j0 = st * kStage;
-        copy_rows<D, kStage, 4>(kb + (uint64_t)j0 * k_row, k_row, keys - j0, at, wave, c);
-        copy_rows<D, kStage, 4>(vb + (uint64_t)j0 * v_row, v_row, keys - j0, at + kStage * G::ROW, wave, c);
+        copy_rows<D, kStage, FEW ? 1 : 4>(kb + (uint64_t)j0 * k_row, k_row, keys - j0, at, FEW ? 0 : wave, c);
+        copy_rows<D, kStage, FEW ? 1 : 4>(vb + (uint64_t)j0 * v_row, v_row, keys - j0, at + kStage * G::ROW, FEW ? 0 : wave, c);
     };
     if (st_begin < st_end) copy_stage(st_begin);
-    float *tab = reinterpret_cast<float *>(lds + kDqLds<D>);
+    float *tab = reinterpret_cast<float *>(lds + (FEW ? kDqFewLds<D> : kDqLds<D>));
     if (BIAS) expand_bias(a, head_kv, tab, 256);
+    if (FEW && BIAS) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wg_barrier();
+    }
 
-    const int v0 = v_wg + wave * 32, v = v0 + (lane & 31);
+    const int v0 = v_wg + (FEW ? 0 : wave * 32), v = v0 + (lane & 31);
     const bool live = v < n_rows;
     const int last = max(min(v0 + 31, n_rows - 1), 0), vc = min(v, last);  // rows behind the last one do its work again, with P = 0
     const int tok = (unsigned)vc / (unsigned)a.group, g = vc - tok * a.group, head = head_kv * a.group + g;
@@ -100,11 +111,21 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     float miss = 0.f;  // sum of dS over this lane's keys
     const float *tab_g = tab + g * a.tab;
     const TileLane<D> t(lane);
-    for (int st = st_begin; st < st_end; ++st) {
-        wait_copies<0>();
-        wg_barrier();
-        if (st + 1 < st_end) copy_stage(st + 1);
-        const char *at = lds + ((st - st_begin) & 1) * (2 * kStage * G::ROW);
+    for (int st = st_begin; st < st_end; st += STRIDE) {
+        if constexpr (FEW) {
+            if (st + STRIDE < st_end) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // nobody waits for this slot's last reads but this wavefront
+                copy_stage(st + STRIDE);
+                wait_copies<2 * G::COPIES>();
+            } else {
+                wait_copies<0>();
+            }
+        } else {
+            wait_copies<0>();
+            wg_barrier();
+            if (st + 1 < st_end) copy_stage(st + 1);
+        }
+        const char *at = ring + ((st - st_begin) / STRIDE & 1) * (2 * kStage * G::ROW);
 #pragma unroll
         for (int h = 0; h < kStage / 32; ++h) {
             const int j0 = st * kStage + 32 * h;
@@ -139,8 +160,39 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
         }
     }
     wait_copies<0>();
-    wg_barrier();
+    if (!FEW) wg_barrier();
     mfma_settle();
+    if constexpr (FEW) {
+        constexpr int PITCH = D + 4;
+        float *mine = reinterpret_cast<float *>(ring) + (lane & 31) * PITCH + 4 * hh, *misses = reinterpret_cast<float *>(lds + 4 * kDqFewRing<D>);
+#pragma unroll
+        for (int dt = 0; dt < G::ND; ++dt)
+#pragma unroll
+            for (int gq = 0; gq < 4; ++gq)
+                *reinterpret_cast<f32x4 *>(mine + 32 * dt + 8 * gq) = f32x4{dq[dt][4 * gq], dq[dt][4 * gq + 1], dq[dt][4 * gq + 2], dq[dt][4 * gq + 3]};
+        miss = half_sum(miss);
+        if (hh == 0) misses[wave * 32 + lane] = miss;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wg_barrier();
+        // (D put right, see below)
+        if (wave == 0 && live && hh == 0)
+            a.aux[(int64_t)head * a.n_q + s.q0 + tok] =
+                make_float2(off, -((misses[lane] + misses[32 + lane]) + (misses[64 + lane] + misses[96 + lane])) - delta);
+        const int row = threadIdx.x / 8, c0 = 4 * (threadIdx.x % 8), to_v = v0 + row;
+        if (to_v >= slot_rows) return;
+        const int to_tok = (unsigned)to_v / (unsigned)a.group, to_head = head_kv * a.group + to_v - to_tok * a.group;
+        uint16_t *dst = a.dq + (s.q0 + to_tok) * a.qs[0] + to_head * a.qs[1] + c0;
+#pragma unroll
+        for (int ch = 0; ch < D; ch += 32) {
+            f32x4 x[4];
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                x[w] = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(lds + w * kDqFewRing<D>) + row * PITCH + c0 + ch);
+            const f32x4 y = ((x[0] + x[1]) + (x[2] + x[3])) * a.scale;
+            *reinterpret_cast<uint2 *>(dst + ch) = to_v < n_rows ? make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])) : make_uint2(0, 0);
+        }
+        return;
+    }
     if (a.parts == 1) {
         store_query_rows<D>(a, s, head_kv, v0, slot_rows, dq, a.scale, live, lds + wave * 32 * G::OUT_ROW, a.dq, a.qs, lane);
     } else if (v < slot_rows) {
@@ -654,14 +706,18 @@ __global__ __launch_bounds__(1024) void attn_sum_bias(AttnArgs a) {
     }
 }
 
-// bytes of LDS of a workgroup of the dK/dV pass' few keys
+// bytes of LDS of a workgroup of few keys, few rows
 template <int D>
-int64_t few_lds(const AttnArgs &a) {
+int64_t few_keys_lds(const AttnArgs &a) {
     return 4 * kFewRing<D> + (a.n_buckets > 0 ? (bias_lds_floats(a) + 4 * (int64_t)a.tab + Skew<kSkew<D>>::BYTES + 4 * a.group * a.n_buckets) * 4 : 0);
+}
+template <int D>
+int64_t few_rows_lds(const AttnArgs &a) {
+    return kDqFewLds<D> + bias_lds_floats(a) * 4;
 }
 struct WsLayout {
     int q_slots, k_slots, q_parts, k_parts;
-    bool few_keys;
+    bool few_rows, few_keys;
     size_t aux, part_q, part_k, part_v, part_bias, total;
 };
 WsLayout layout(const AttnArgs &a, int d) {
@@ -670,22 +726,31 @@ WsLayout layout(const AttnArgs &a, int d) {
     w.q_slots = (int)(rows / 128 + a.n_seq);
     w.k_slots = a.n_k / 128 + a.n_seq;
     const double steps = walk_steps(a), full = full_chip(d);
-    w.q_parts = best_parts(steps, d == 32 ? 450 : d == 64 ? 600 : 1050, ((double)rows / 128 + 1) * a.h_kv, full, (double)a.n_q * a.h_q * d * 8,
-                           (int64_t)a.n_k / a.n_seq / 32, (int64_t)w.q_slots * a.h_kv);
-    const double k_cycles = d == 32 ? 600 : d == 64 ? 800 : 1400, k_wgs = ((double)a.n_k / 128 + 1) * a.h_kv;
-    const int64_t walk = rows / a.n_seq / 32, slots32 = a.n_k / 32 + a.n_seq;
-    double cut, few;
-    w.k_parts = best_parts(steps, k_cycles, k_wgs, full, (double)a.n_k * a.h_kv * d * 16, walk, (int64_t)w.k_slots * a.h_kv, &cut);
-    // 32 keys to a workgroup: where those are all on the chip at the same time, and cutting the walks of 128 does not promise more.  Neither takes less
-    // than the steps behind each other in its longest walks, at about twice the cycles of a step on a full chip.
-    best_parts(steps, k_cycles, 4 * k_wgs, full, 0, 0, 0, &few);
-    const double chain = walk * k_cycles * 2 / 2.1e3;
-    few = std::max(few, chain / 4);
-    cut = std::max(cut, chain / w.k_parts + (w.k_parts > 1 ? 4 : 0));
-    const int64_t lds = d == 32 ? few_lds<32>(a) : d == 64 ? few_lds<64>(a) : few_lds<128>(a);
-    w.few_keys = slots32 * a.h_kv <= (d == 128 ? 256 : 512) && lds <= 160 * 1024 && few <= cut;
+    // Tiles of 128 rows (keys), their walks cut into parts where there are few, or tiles of 32: where those are all on the chip at the same time,
+    // and the cutting does not promise more.  Neither takes less than the steps behind each other in its longest walks, at about
+    // twice the cycles of a step on a full chip.
+    auto choose = [&](double cycles, double wgs, double bytes, int64_t walk, int64_t grid, int64_t slots32, int64_t lds, int &parts) {
+        double cut, few;
+        parts = best_parts(steps, cycles, wgs, full, bytes, walk, grid, &cut);
+        best_parts(steps, cycles, 4 * wgs, full, 0, 0, 0, &few);
+        const double chain = walk * cycles * 2 / 2.1e3;
+        few = std::max(few, chain / 4);
+        cut = std::max(cut, chain / parts + (parts > 1 ? 4 : 0));
+        return slots32 * a.h_kv <= (d == 128 ? 256 : 512) && lds <= 160 * 1024 && few <= cut;
+    };
+    const int64_t rows32 = rows / 32 + a.n_seq, keys32 = a.n_k / 32 + a.n_seq;
+    const int64_t rows_lds = d == 32 ? few_rows_lds<32>(a) : d == 64 ? few_rows_lds<64>(a) : few_rows_lds<128>(a);
+    const int64_t keys_lds = d == 32 ? few_keys_lds<32>(a) : d == 64 ? few_keys_lds<64>(a) : few_keys_lds<128>(a);
+    w.few_rows = choose(d == 32 ? 450 : d == 64 ? 600 : 1050, ((double)rows / 128 + 1) * a.h_kv, (double)a.n_q * a.h_q * d * 8,
+                        (int64_t)a.n_k / a.n_seq / 32, (int64_t)w.q_slots * a.h_kv, rows32, rows_lds, w.q_parts);
+    w.few_keys = choose(d == 32 ? 600 : d == 64 ? 800 : 1400, ((double)a.n_k / 128 + 1) * a.h_kv, (double)a.n_k * a.h_kv * d * 16, rows / a.n_seq / 32,
+                        (int64_t)w.k_slots * a.h_kv, keys32, keys_lds, w.k_parts);
+    if (w.few_rows) {
+        w.q_slots = (int)rows32;
+        w.q_parts = 1;
+    }
     if (w.few_keys) {
-        w.k_slots = (int)slots32;
+        w.k_slots = (int)keys32;
         w.k_parts = 1;
     }
     size_t at = 0;
@@ -716,13 +781,18 @@ lsrm_status launch_backward_d(AttnArgs a, void *ws, hipStream_t st) {
         a.part_bias = a.dbias != nullptr ? reinterpret_cast<float *>(base + w.part_bias) : nullptr;
         const int n_tab = bias_lds_floats(a) * 4;
         a.parts = w.q_parts;
-        lsrm_status rc = launch_attn(bias ? &attn_dq_kernel<D, true> : &attn_dq_kernel<D, false>, (int64_t)w.q_slots * a.h_kv * w.q_parts, 256,
-                                     kDqLds<D> + n_tab, a, st);
+        lsrm_status rc;
+        if (w.few_rows)
+            rc = launch_attn(bias ? &attn_dq_kernel<D, true, true> : &attn_dq_kernel<D, false, true>, (int64_t)w.q_slots * a.h_kv, 256,
+                             (int)few_rows_lds<D>(a), a, st);
+        else
+            rc = launch_attn(bias ? &attn_dq_kernel<D, true, false> : &attn_dq_kernel<D, false, false>, (int64_t)w.q_slots * a.h_kv * w.q_parts, 256,
+                             kDqLds<D> + n_tab, a, st);
         if (rc != LSRM_OK) return rc;
         if (w.q_parts > 1 && (rc = launch_attn(&attn_sum_parts<D, true>, ((int64_t)a.n_q / (2048 / D) + a.n_seq) * a.h_q, 256, 0, a, st)) != LSRM_OK) return rc;
         a.parts = w.k_parts;
         if (w.few_keys)
-            rc = launch_attn(bias ? &attn_dkv_kernel<D, true, true> : &attn_dkv_kernel<D, false, true>, (int64_t)w.k_slots * a.h_kv, 256, (int)few_lds<D>(a), a, st);
+            rc = launch_attn(bias ? &attn_dkv_kernel<D, true, true> : &attn_dkv_kernel<D, false, true>, (int64_t)w.k_slots * a.h_kv, 256, (int)few_keys_lds<D>(a), a, st);
         else
             rc = launch_attn(bias ? &attn_dkv_kernel<D, true, false> : &attn_dkv_kernel<D, false, false>, (int64_t)w.k_slots * a.h_kv * w.k_parts, 256,
                              kDkvLds<D> + kDkvValues<D> + (bias ? n_tab + 32 + (a.dbias != nullptr ? 16 * a.tab + 4 * Skew<kSkew<D>>::BYTES : 0) : 0), a, st);
