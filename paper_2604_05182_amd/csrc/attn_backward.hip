@@ -726,31 +726,35 @@ WsLayout layout(const AttnArgs &a, int d) {
     w.q_slots = (int)(rows / 128 + a.n_seq);
     w.k_slots = a.n_k / 128 + a.n_seq;
     const double steps = walk_steps(a), full = full_chip(d);
-    // Tiles of 128 rows (keys), their walks cut into parts where there are few, or tiles of 32: where those are all on the chip at the same time,
-    // and the cutting does not promise more.  Neither takes less than the steps behind each other in its longest walks, at about
-    // twice the cycles of a step on a full chip.
-    auto choose = [&](double cycles, double wgs, double bytes, int64_t walk, int64_t grid, int64_t slots32, int64_t lds, int &parts) {
+    // Tiles of 128 rows (keys), their walks cut into parts where there are few, or tiles of 32 with the walks dealt to four wavefronts: what promises to
+    // be done first.  Neither takes less than the steps behind each other in its walks, at about twice the cycles of a step on a full chip; for tiles of
+    // 32 two steps more, where the wavefronts' sums meet, and all of it as often as the chip has to be filled (with two workgroups to a CU), which they
+    // are not for more than two times: each tile is copied for 32 rows instead of 128, at least a fifth of the time on a full chip.
+    // Backward, with 128 keys and rows and with 32: 4 x 512 tokens, causal, 8 heads on 4, d = 64 41.8 and 21.8 us, d = 128 66.4 and 41.6; 32 x 64 tokens,
+    // 8 heads of 64 (walks of two steps), 15.6 and 21.0; 8 x 900 tokens, 8 heads of 32 (four times the chip), 54 and 62.
+    auto choose = [&](double cycles, int64_t n, double bytes, int64_t walk, int64_t grid, int64_t lds, int &parts) {
+        const double wgs = ((double)n / 128 + 1) * a.h_kv, step = cycles * 2 / 2.1e3;
         double cut, few;
         parts = best_parts(steps, cycles, wgs, full, bytes, walk, grid, &cut);
         best_parts(steps, cycles, 4 * wgs, full, 0, 0, 0, &few);
-        const double chain = walk * cycles * 2 / 2.1e3;
-        few = std::max(few, chain / 4);
-        cut = std::max(cut, chain / parts + (parts > 1 ? 4 : 0));
-        return slots32 * a.h_kv <= (d == 128 ? 256 : 512) && lds <= 160 * 1024 && few <= cut;
+        const int64_t at_once = 256 * std::min<int64_t>(2, 160 * 1024 / lds);
+        const int64_t times = at_once > 0 ? (n / 32 * a.h_kv + at_once - 1) / at_once : 3;
+        few = std::max(1.2 * few, step * ((walk + 3) / 4 + 2) * times);
+        cut = std::max(cut, step * walk / parts + (parts > 1 ? 4 : 0));
+        return times <= 2 && few <= cut;
     };
-    const int64_t rows32 = rows / 32 + a.n_seq, keys32 = a.n_k / 32 + a.n_seq;
     const int64_t rows_lds = d == 32 ? few_rows_lds<32>(a) : d == 64 ? few_rows_lds<64>(a) : few_rows_lds<128>(a);
     const int64_t keys_lds = d == 32 ? few_keys_lds<32>(a) : d == 64 ? few_keys_lds<64>(a) : few_keys_lds<128>(a);
-    w.few_rows = choose(d == 32 ? 450 : d == 64 ? 600 : 1050, ((double)rows / 128 + 1) * a.h_kv, (double)a.n_q * a.h_q * d * 8,
-                        (int64_t)a.n_k / a.n_seq / 32, (int64_t)w.q_slots * a.h_kv, rows32, rows_lds, w.q_parts);
-    w.few_keys = choose(d == 32 ? 600 : d == 64 ? 800 : 1400, ((double)a.n_k / 128 + 1) * a.h_kv, (double)a.n_k * a.h_kv * d * 16, rows / a.n_seq / 32,
-                        (int64_t)w.k_slots * a.h_kv, keys32, keys_lds, w.k_parts);
+    w.few_rows = choose(d == 32 ? 450 : d == 64 ? 600 : 1050, rows, (double)a.n_q * a.h_q * d * 8, (int64_t)a.n_k / a.n_seq / 32,
+                        (int64_t)w.q_slots * a.h_kv, rows_lds, w.q_parts);
+    w.few_keys = choose(d == 32 ? 600 : d == 64 ? 800 : 1400, a.n_k, (double)a.n_k * a.h_kv * d * 16, rows / a.n_seq / 32,
+                        (int64_t)w.k_slots * a.h_kv, keys_lds, w.k_parts);
     if (w.few_rows) {
-        w.q_slots = (int)rows32;
+        w.q_slots = (int)(rows / 32 + a.n_seq);
         w.q_parts = 1;
     }
     if (w.few_keys) {
-        w.k_slots = (int)keys32;
+        w.k_slots = a.n_k / 32 + a.n_seq;
         w.k_parts = 1;
     }
     size_t at = 0;

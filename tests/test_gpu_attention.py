@@ -530,9 +530,11 @@ def test_one_row_of_a_large_cache(B):
 @pytest.mark.parametrize("case", [
     dict(q_lens=[257, 100, 30, 1, 180], h=8, hk=4),               # few keys to a workgroup
     dict(q_lens=[1, 40, 0, 5], k_lens=[33, 0, 64, 200], h=6, hk=1),  # the same; fewer tiles of queries than wavefronts, none at all
-    dict(q_lens=[300, 260], h=32),                                # many
-    dict(q_lens=[2048], h=8, hk=2),                               # many, walks cut
-], ids=["few", "few, short", "many", "many, cut"])
+    dict(q_lens=[640, 520], h=32),                                # 128 rows and keys
+    dict(q_lens=[2048], h=8, hk=2),                               # dK, dV: walks cut
+    dict(q_lens=[70], k_lens=[6000], h=2, hk=1),                  # dQ: walks cut
+    dict(q_lens=[6000], k_lens=[70], h=2, hk=1),
+], ids=["few", "few, short", "many", "grouped", "few queries", "few keys"])
 def test_every_way_backward(B, case, bias, causal, d):
     x = Problem(B, d=d, causal=causal, seed=103, slots=9, edge=3, bounds=[-90, -17, -1, 0, 1, 40] if bias else None, **case)
     x.forward()
